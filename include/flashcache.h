@@ -360,6 +360,101 @@ fc_status fc_decode_attention(fc_handle *h, const fc_decode_args *a, void *out,
                               void *workspace, size_t workspace_bytes, fc_stream stream);
 
 /*
+ * A cache held in 4 bits.  Every row of a head (K and V alike) is two halves of head_dim/2 channels; a half has a scale and
+ * a minimum of the cache's 16-bit type and a code 0..15 per channel, which stands for  minimum + scale * code:
+ * head_dim/2 + 8 bytes instead of 2*head_dim.  The order of the codes inside a row is the decoding kernel's own (the four
+ * functions below agree on it; fc_cache4.cuh has it).
+ *
+ *   codes_k/v     DEVICE [num_heads][capacity_rows][head_dim/2] bytes
+ *   params_k/v    DEVICE [num_heads][capacity_rows][4] of dtype: (scale, minimum) of either half
+ *   capacity_rows a multiple of 16; all pointers 16-byte aligned
+ *   dtype FC_F16 or FC_BF16, head_dim 64 or 128
+ */
+typedef struct {
+  void *codes_k, *codes_v;
+  void *params_k, *params_v;
+  int64_t capacity_rows;
+  int32_t dtype, num_heads, head_dim;
+} fc_cache4;
+
+/*
+ * Rows of K and V (a compacted cache as fc_select_compact leaves it, or any view) into 4 bits.  Per half row the scale is
+ * (max - min) / 15, rounded up to dtype, so that no value moves by more than half a step; the code is (x - min) / scale to
+ * the nearest whole number, the even one of two equally near, decided exactly.  A half with a value that is not finite, or
+ * whose range is past fp32, stands for NaN in every channel.  Rows of the cache that are not named stay as they are.
+ *
+ *   kv         the rows: cu_seqlens[batch] of them, how they split into sequences does not matter
+ *   used       DEVICE int64 or NULL: only the first min(*used, cu_seqlens[batch]) rows are taken (the last entry of a
+ *              layer's out_offsets: how many rows the layer kept is known on the device first)
+ *   out_rows   DEVICE int64[rows] or NULL (row i goes to row i): the cache row each row goes to; a negative one is left
+ *              out, one past the capacity too, with FC_ERR_INTERNAL in the status word.  The same row named twice gets one
+ *              of the two, which one is open (and codes and scales may then be of different ones).
+ * Errors: FC_ERR_INVALID_ARG (also: view and cache of different dtype, heads or head_dim), FC_ERR_UNSUPPORTED, FC_ERR_CUDA.
+ */
+fc_status fc_quantize_cache(fc_handle *h, const fc_kv_view *kv, const fc_cache4 *cache, const int64_t *used,
+                            const int64_t *out_rows, fc_stream stream);
+/* The values the first min(*used, rows) rows stand for, rounded once to dtype: out_k, out_v DEVICE dense
+ * [rows][num_heads][head_dim]; rows behind them are left as they are. */
+fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k, void *out_v, int64_t rows,
+                              const int64_t *used, fc_stream stream);
+
+/*
+ * Rotary positions.  The first rotary_dim channels of a head are rotary_dim/2 pairs, (j, j + rotary_dim/2) or, interleaved,
+ * (2j, 2j+1); pair j of a token at position p turns by p * freq[j]:
+ *     (a, b) -> (a c - b s, b c + a s),  c = scale*cos, s = scale*sin  (inverse: s = -scale*sin; with scale 1 this undoes
+ *     the rotation, and for any scale it is its gradient).
+ * The other channels are copied.  Angles are taken in fp64 and reduced by whole turns before they are rounded to fp32.
+ *
+ *   q, out_q, k, out_k   DEVICE, either pair may be NULL; strides in elements, rows 16-byte aligned, channel stride 1.  An
+ *                        output may be its input with the same strides (without out_rows); no other overlap.
+ *   v, out_v     DEVICE or NULL: values laid out like k and out_k, copied beside the keys (the append of a decoding step)
+ *   out_rows     DEVICE int64[tokens] or NULL: row of out_k and out_v each token's key and value go to (b * tail_capacity +
+ *                tail_len[b] in a decoding tail).  Negative: left out (padding).  >= out_capacity_rows: left out, and
+ *                FC_ERR_INTERNAL in the status word.  No row may be named twice.
+ *   positions    DEVICE int64[axes][position_stride]: one axis, or three (time, height, width) where `sections` says how
+ *                many pairs, from the first on, turn by each axis (their sum is rotary_dim/2; all 0: one axis)
+ *   freq         HOST double[rotary_dim/2], radians per position (fc_rotary_frequencies); read during the call
+ * Limits: FC_F32, FC_F16 or FC_BF16; head_dim a multiple of 64 up to 1024, rotary_dim even, at most min(head_dim, 256).
+ */
+typedef struct {
+  const void *q;
+  void *out_q;
+  int64_t q_stride_token, q_stride_head, out_q_stride_token, out_q_stride_head;
+  const void *k;
+  void *out_k;
+  int64_t k_stride_token, k_stride_head, out_k_stride_token, out_k_stride_head;
+  const void *v;
+  void *out_v;
+  const int64_t *out_rows;
+  int64_t out_capacity_rows;
+  const int64_t *positions;
+  int64_t position_stride, tokens;
+  const double *freq;
+  double scale;
+  int32_t dtype, num_q_heads, num_heads, head_dim, rotary_dim, interleaved, inverse;
+  int32_t sections[3];
+} fc_rotary_args;
+
+fc_status fc_rotary(fc_handle *h, const fc_rotary_args *a, fc_stream stream);
+
+/* Frequencies for fc_rotary, f_j = base^(-2j/rotary_dim), and the factor on cosine and sine (1 except for FC_ROPE_YARN).
+ * Scaled for contexts longer than the trained ones by factor >= 1 (sc == NULL: FC_ROPE_PLAIN):
+ *   FC_ROPE_LINEAR  f_j / factor
+ *   FC_ROPE_NTK     base * factor^(rotary_dim/(rotary_dim-2)) as base
+ *   FC_ROPE_YARN    pairs of more than `high` turns over original_len tokens keep f_j, of fewer than `low` get f_j / factor,
+ *                   a line in between (over the pair's index); scale = 0.1 ln(factor) + 1.  Usual: low 1, high 32
+ *   FC_ROPE_BANDS   the same with the line over the number of turns, scale 1.  Usual: low 1, high 4
+ * Host only, nothing is launched. */
+typedef enum { FC_ROPE_PLAIN = 0, FC_ROPE_LINEAR = 1, FC_ROPE_NTK = 2, FC_ROPE_YARN = 3, FC_ROPE_BANDS = 4 } fc_rope_kind;
+typedef struct {
+  int32_t kind;
+  double factor;
+  int64_t original_len;
+  double low, high;
+} fc_rope_scaling;
+fc_status fc_rotary_frequencies(int32_t rotary_dim, double base, const fc_rope_scaling *sc, double *freq, double *scale);
+
+/*
  * fc_select_compact with options (opt == NULL: exactly fc_select_compact).
  *
  *   per_layer  0: every KV head keeps its own tokens (the default reading: Eq. 10 over the head's

@@ -30,6 +30,7 @@ EXPORTS = (
     "fc_select_compact_layers", "fc_layer_capacity_rows", "fc_score_layers", "fc_score_layers_workspace_bytes",
     "fc_power_spectrum_workspace_bytes", "fc_power_spectrum", "fc_cutoff_from_spectrum",
     "fc_decode_workspace_bytes", "fc_decode_attention",
+    "fc_quantize_cache", "fc_dequantize_cache", "fc_rotary", "fc_rotary_frequencies",
     "fc_static_scratch_bytes", "fc_score_layer_static", "fc_static_last_device_status",
     "fc_compress_host_rows", "fc_compress_host_arena_bytes", "fc_compress_host",
 )
@@ -60,6 +61,29 @@ class fc_decode_args(ctypes.Structure):
         ("tail_capacity", c_int32), ("dtype", c_int32), ("batch", c_int32), ("num_heads", c_int32),
         ("num_q_heads", c_int32), ("head_dim", c_int32), ("max_rows", c_int64),
     ]
+
+
+class fc_cache4(ctypes.Structure):
+    _fields_ = [("codes_k", c_void_p), ("codes_v", c_void_p), ("params_k", c_void_p), ("params_v", c_void_p),
+                ("capacity_rows", c_int64), ("dtype", c_int32), ("num_heads", c_int32), ("head_dim", c_int32)]
+
+
+class fc_rotary_args(ctypes.Structure):
+    _fields_ = [
+        ("q", c_void_p), ("out_q", c_void_p),
+        ("q_stride_token", c_int64), ("q_stride_head", c_int64), ("out_q_stride_token", c_int64), ("out_q_stride_head", c_int64),
+        ("k", c_void_p), ("out_k", c_void_p),
+        ("k_stride_token", c_int64), ("k_stride_head", c_int64), ("out_k_stride_token", c_int64), ("out_k_stride_head", c_int64),
+        ("v", c_void_p), ("out_v", c_void_p), ("out_rows", c_void_p), ("out_capacity_rows", c_int64),
+        ("positions", c_void_p), ("position_stride", c_int64), ("tokens", c_int64),
+        ("freq", POINTER(c_double)), ("scale", c_double),
+        ("dtype", c_int32), ("num_q_heads", c_int32), ("num_heads", c_int32), ("head_dim", c_int32), ("rotary_dim", c_int32),
+        ("interleaved", c_int32), ("inverse", c_int32), ("sections", c_int32 * 3),
+    ]
+
+
+class fc_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", c_int32), ("factor", c_double), ("original_len", c_int64), ("low", c_double), ("high", c_double)]
 
 
 class fc_host_job(ctypes.Structure):
@@ -170,6 +194,14 @@ def _load() -> ctypes.CDLL:
     lib.fc_decode_workspace_bytes.restype = c_size_t
     lib.fc_decode_attention.argtypes = [c_void_p, POINTER(fc_decode_args), c_void_p, c_void_p, c_size_t, c_void_p]
     lib.fc_decode_attention.restype = c_int
+    lib.fc_quantize_cache.argtypes = [c_void_p, POINTER(fc_kv_view), POINTER(fc_cache4), c_void_p, c_void_p, c_void_p]
+    lib.fc_quantize_cache.restype = c_int
+    lib.fc_dequantize_cache.argtypes = [c_void_p, POINTER(fc_cache4), c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
+    lib.fc_dequantize_cache.restype = c_int
+    lib.fc_rotary.argtypes = [c_void_p, POINTER(fc_rotary_args), c_void_p]
+    lib.fc_rotary.restype = c_int
+    lib.fc_rotary_frequencies.argtypes = [c_int32, c_double, POINTER(fc_rope_scaling), POINTER(c_double), POINTER(c_double)]
+    lib.fc_rotary_frequencies.restype = c_int
     lib.fc_static_scratch_bytes.argtypes = []
     lib.fc_static_scratch_bytes.restype = c_size_t
     lib.fc_score_layer_static.argtypes = [POINTER(fc_kv_view), c_double, c_void_p, c_void_p, c_void_p]
@@ -439,6 +471,163 @@ def fc_decode_attention(handle, args, out, workspace) -> None:
     rc = _lib.fc_decode_attention(handle, byref(args), out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream())
     if rc != FC_OK:
         raise FlashCacheError(rc, "fc_decode_attention")
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    """The current stream of the device that `t` lives on, which need not be the current device."""
+    if _raw_stream is not None:
+        return _raw_stream(t.device.index)
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _same_device(*tensors) -> None:
+    at = {t.device for t in tensors if t is not None}
+    if len(at) != 1 or next(iter(at)).type != "cuda":
+        raise ValueError("tensors of one CUDA device: got %s" % ", ".join(sorted(map(str, at))))
+
+
+def _counter(t, what: str, numel: int | None = None) -> None:
+    if t is not None and (t.dtype != torch.int64 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
+        raise ValueError("%s: contiguous int64 device tensor%s" % (what, "" if numel is None else " of %d" % numel))
+
+
+class Cache4:
+    """A cache held in 4 bits (fc_cache4): uint8 codes [H, capacity, d/2] and parameters [H, capacity, 4] of the 16-bit type, of K
+    and of V.  `Cache4.empty` allocates one."""
+
+    def __init__(self, codes_k, codes_v, params_k, params_v):
+        H, cap, half = (int(x) for x in codes_k.shape)
+        for c in (codes_k, codes_v):
+            if c.dtype != torch.uint8 or tuple(c.shape) != (H, cap, half) or not c.is_contiguous():
+                raise ValueError("codes_k/codes_v: contiguous uint8 [H, capacity, d/2]")
+        for p in (params_k, params_v):
+            if p.dtype != params_k.dtype or p.dtype not in _DTYPE or tuple(p.shape) != (H, cap, 4) or not p.is_contiguous():
+                raise ValueError("params_k/params_v: contiguous [H, capacity, 4] of the cache's 16-bit type")
+        _same_device(codes_k, codes_v, params_k, params_v)
+        self.codes_k, self.codes_v, self.params_k, self.params_v = codes_k, codes_v, params_k, params_v
+        self.num_heads, self.capacity_rows, self.head_dim, self.dtype = H, cap, 2 * half, params_k.dtype
+        self.c = fc_cache4(codes_k.data_ptr(), codes_v.data_ptr(), params_k.data_ptr(), params_v.data_ptr(), cap,
+                           _DTYPE[self.dtype], H, self.head_dim)
+
+    @classmethod
+    def empty(cls, rows: int, num_heads: int, head_dim: int, dtype, device="cuda") -> "Cache4":
+        """Room for at least `rows` rows (the capacity is the next multiple of 16)."""
+        cap = max(16, (int(rows) + 15) // 16 * 16)
+        codes = [torch.empty((num_heads, cap, head_dim // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*codes, *[torch.empty((num_heads, cap, 4), dtype=dtype, device=device) for _ in range(2)])
+
+    @property
+    def nbytes(self) -> int:
+        return sum(t.nbytes for t in (self.codes_k, self.codes_v, self.params_k, self.params_v))
+
+
+def fc_quantize_cache(handle, k, v, cache: Cache4, used=None, out_rows=None) -> None:
+    """Rows k, v [rows, H, d] into 4 bits.  used: int64 [1] on the device, how many of them; out_rows: int64 [rows] on the device,
+    the cache row each goes to (negative: left out)."""
+    rows = int(k.shape[0])
+    cu = (c_int32 * 2)(0, rows)
+    view = make_view(k, v, cu)
+    _same_device(k, v, cache.codes_k, used, out_rows)
+    _counter(used, "used", 1)
+    _counter(out_rows, "out_rows", rows)
+    _check(_lib.fc_quantize_cache(handle, byref(view), byref(cache.c), used.data_ptr() if used is not None else None,
+                                  out_rows.data_ptr() if out_rows is not None else None, _stream_of(k)), "fc_quantize_cache")
+
+
+def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
+    """The values the first rows of the cache stand for into out_k, out_v [rows, H, d] (`used`: as in fc_quantize_cache)."""
+    rows = int(out_k.shape[0])
+    for o in (out_k, out_v):
+        if tuple(o.shape) != (rows, cache.num_heads, cache.head_dim) or o.dtype != cache.dtype or not o.is_contiguous():
+            raise ValueError("out_k/out_v: contiguous [rows, H, d] of the cache's type")
+    _same_device(out_k, out_v, cache.codes_k, used)
+    _counter(used, "used", 1)
+    _check(_lib.fc_dequantize_cache(handle, byref(cache.c), out_k.data_ptr(), out_v.data_ptr(), rows,
+                                    used.data_ptr() if used is not None else None, _stream_of(out_k)), "fc_dequantize_cache")
+
+
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+_ROPE_HIGH = {"yarn": 32.0, "bands": 4.0}
+
+
+def fc_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: int = 0,
+                          low: float = 1.0, high: float | None = None):
+    """-> (frequencies in radians per position, the factor on cosine and sine).  scaling: "none", "linear", "ntk", "yarn" or
+    "bands"; low, high: numbers of turns over original_len between which frequencies go from scaled to kept (yarn, bands)."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError("scaling: one of %s" % ", ".join(ROPE_SCALING))
+    high = _ROPE_HIGH.get(scaling, 2.0) if high is None else high
+    sc = fc_rope_scaling(ROPE_SCALING[scaling], float(factor), int(original_len), float(low), float(high))
+    freq, scale = (c_double * max(1, int(rotary_dim) // 2))(), c_double(1.0)
+    _check(_lib.fc_rotary_frequencies(int(rotary_dim), float(base), byref(sc), freq, byref(scale)), "fc_rotary_frequencies")
+    return list(freq), float(scale.value)
+
+
+def _row_strides(t, name: str):
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError("%s: [tokens, heads, d] with channel stride 1" % name)
+    return t.stride(0), t.stride(1)
+
+
+def make_rotary_args(positions, freq, q=None, out_q=None, k=None, out_k=None, v=None, out_v=None, out_rows=None, scale: float = 1.0,
+                     interleaved: bool = False, inverse: bool = False, sections=None):
+    """positions: int64 [T], or [axes, T] with `sections` (three numbers of pairs); freq: from fc_rotary_frequencies (its length is
+    half the rotated channels).  q [T, Hq, d] -> out_q, k [T, H, d] -> out_k; v -> out_v as it is.  out_rows: int64 [T], the rows of
+    out_k and out_v (negative: left out).  The arguments hold pointers: keep the tensors."""
+    rows = q if q is not None else k
+    if rows is None:
+        raise ValueError("q or k, or both")
+    if positions.dim() == 1:
+        positions = positions.unsqueeze(0)
+    T, d = int(rows.shape[0]), int(rows.shape[2])
+    axes = 3 if sections is not None else 1
+    if positions.dtype != torch.int64 or tuple(positions.shape) != (axes, T) or (T > 1 and positions.stride(1) != 1):
+        raise ValueError("positions: int64 [T], or [3, T] with sections")
+    a = fc_rotary_args(positions=positions.data_ptr(), position_stride=positions.stride(0), tokens=T, scale=float(scale),
+                       dtype=_DTYPE[rows.dtype], head_dim=d, rotary_dim=2 * len(freq), interleaved=1 if interleaved else 0,
+                       inverse=1 if inverse else 0)
+    table = (c_double * len(freq))(*[float(f) for f in freq])
+    a.freq = ctypes.cast(table, POINTER(c_double))
+    if sections is not None:
+        a.sections = (c_int32 * 3)(*[int(x) for x in sections])
+    for x, out in ((q, out_q), (k, out_k), (v, out_v)):
+        if (x is None) != (out is None):
+            raise ValueError("every input with its output")
+        if x is not None and (x.dtype != rows.dtype or out.dtype != rows.dtype or int(x.shape[0]) != T or x.shape[2] != d
+                              or out.shape[1:] != x.shape[1:]):
+            raise ValueError("q, k, v and their outputs: [T, heads, d] of one dtype")
+    if q is not None:
+        if out_q.shape[0] != T:
+            raise ValueError("out_q: laid out like q")
+        a.q, a.out_q, a.num_q_heads = q.data_ptr(), out_q.data_ptr(), int(q.shape[1])
+        a.q_stride_token, a.q_stride_head = _row_strides(q, "q")
+        a.out_q_stride_token, a.out_q_stride_head = _row_strides(out_q, "out_q")
+    if k is not None:
+        if out_rows is None and out_k.shape[0] != T:
+            raise ValueError("out_k: T rows, or out_rows")
+        a.k, a.out_k, a.num_heads = k.data_ptr(), out_k.data_ptr(), int(k.shape[1])
+        a.k_stride_token, a.k_stride_head = _row_strides(k, "k")
+        a.out_k_stride_token, a.out_k_stride_head = _row_strides(out_k, "out_k")
+        a.out_capacity_rows = int(out_k.shape[0])
+    if v is not None:
+        if k is None or v.shape != k.shape or v.stride() != k.stride() or out_v.shape != out_k.shape or out_v.stride() != out_k.stride():
+            raise ValueError("v and out_v: laid out like k and out_k")
+        a.v, a.out_v = v.data_ptr(), out_v.data_ptr()
+    if out_rows is not None:
+        if k is None:
+            raise ValueError("out_rows: rows of out_k")
+        _counter(out_rows, "out_rows", T)
+        a.out_rows = out_rows.data_ptr()
+    _same_device(positions, q, out_q, k, out_k, v, out_v, out_rows)
+    a._kept = table
+    a._device = rows
+    return a
+
+
+def fc_rotary(handle, args) -> None:
+    rc = _lib.fc_rotary(handle, byref(args), _stream_of(args._device))
+    if rc != FC_OK:
+        raise FlashCacheError(rc, "fc_rotary")
 
 
 def fc_reset_ordering(handle) -> None:

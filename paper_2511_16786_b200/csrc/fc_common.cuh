@@ -537,6 +537,24 @@ inline fc_status fc_after_launch(fc_handle *h) {
   return cudaGetLastError() == cudaSuccess ? FC_OK : FC_ERR_CUDA;
 }
 
+// The handle's device for the length of a call; the caller's is current again afterwards.  It is always set, not only where
+// it differs: in a thread that has made no CUDA call yet device 0 is current but no context is.
+struct FcDeviceGuard {
+  int before;
+  bool ok;
+  explicit FcDeviceGuard(int device) : before(-1), ok(false) {
+    if (cudaGetDevice(&before) != cudaSuccess) before = -1;
+    ok = cudaSetDevice(device) == cudaSuccess;
+    if (!ok) cudaGetLastError();
+    if (before == device) before = -1;
+  }
+  ~FcDeviceGuard() {
+    if (before >= 0 && cudaSetDevice(before) != cudaSuccess) cudaGetLastError();
+  }
+  FcDeviceGuard(const FcDeviceGuard &) = delete;
+  FcDeviceGuard &operator=(const FcDeviceGuard &) = delete;
+};
+
 // Shared claim on the context's persisting-L2 limit (fc_api.cu).
 bool fc_persist_acquire(fc_handle *h);
 void fc_persist_release(fc_handle *h);
