@@ -399,6 +399,25 @@ fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k,
                               const int64_t *used, fc_stream stream);
 
 /*
+ * fc_decode_attention with options (opt == NULL: exactly fc_decode_attention; else head_dim 64 or 128).
+ *
+ *   cache4    NULL: the kept rows are args' cache_k and cache_v.  Else they are held in 4 bits and args' cache_k, cache_v
+ *             and cache_rows are not read; dtype, num_heads and head_dim are args'.  The tail is in 16 bits either way.
+ *             Sums and softmax statistics in fp32; a weight is rounded to fp16 (11 bits) once, beside its row's scale.
+ *   window    0: every row is visible.  Else, of a sequence's n rows (kept ones, then the tail), only the last `window`
+ *   sinks     and the first `sinks` are; the others are not read (whole tiles of them).
+ * Rows without weight (outside the window, or past a sequence's end) may hold anything.  A sequence without rows gives zeros.
+ */
+typedef struct {
+  const fc_cache4 *cache4;
+  int32_t window, sinks;
+} fc_decode_options;
+
+size_t fc_decode_workspace_bytes_ex(const fc_handle *h, const fc_decode_args *a, const fc_decode_options *opt);
+fc_status fc_decode_attention_ex(fc_handle *h, const fc_decode_args *a, const fc_decode_options *opt, void *out,
+                                 void *workspace, size_t workspace_bytes, fc_stream stream);
+
+/*
  * Rotary positions.  The first rotary_dim channels of a head are rotary_dim/2 pairs, (j, j + rotary_dim/2) or, interleaved,
  * (2j, 2j+1); pair j of a token at position p turns by p * freq[j]:
  *     (a, b) -> (a c - b s, b c + a s),  c = scale*cos, s = scale*sin  (inverse: s = -scale*sin; with scale 1 this undoes

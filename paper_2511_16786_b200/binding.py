@@ -30,6 +30,7 @@ EXPORTS = (
     "fc_select_compact_layers", "fc_layer_capacity_rows", "fc_score_layers", "fc_score_layers_workspace_bytes",
     "fc_power_spectrum_workspace_bytes", "fc_power_spectrum", "fc_cutoff_from_spectrum",
     "fc_decode_workspace_bytes", "fc_decode_attention",
+    "fc_decode_workspace_bytes_ex", "fc_decode_attention_ex",
     "fc_quantize_cache", "fc_dequantize_cache", "fc_rotary", "fc_rotary_frequencies",
     "fc_static_scratch_bytes", "fc_score_layer_static", "fc_static_last_device_status",
     "fc_compress_host_rows", "fc_compress_host_arena_bytes", "fc_compress_host",
@@ -66,6 +67,10 @@ class fc_decode_args(ctypes.Structure):
 class fc_cache4(ctypes.Structure):
     _fields_ = [("codes_k", c_void_p), ("codes_v", c_void_p), ("params_k", c_void_p), ("params_v", c_void_p),
                 ("capacity_rows", c_int64), ("dtype", c_int32), ("num_heads", c_int32), ("head_dim", c_int32)]
+
+
+class fc_decode_options(ctypes.Structure):
+    _fields_ = [("cache4", POINTER(fc_cache4)), ("window", c_int32), ("sinks", c_int32)]
 
 
 class fc_rotary_args(ctypes.Structure):
@@ -198,6 +203,11 @@ def _load() -> ctypes.CDLL:
     lib.fc_quantize_cache.restype = c_int
     lib.fc_dequantize_cache.argtypes = [c_void_p, POINTER(fc_cache4), c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
     lib.fc_dequantize_cache.restype = c_int
+    lib.fc_decode_workspace_bytes_ex.argtypes = [c_void_p, POINTER(fc_decode_args), POINTER(fc_decode_options)]
+    lib.fc_decode_workspace_bytes_ex.restype = c_size_t
+    lib.fc_decode_attention_ex.argtypes = [c_void_p, POINTER(fc_decode_args), POINTER(fc_decode_options), c_void_p, c_void_p,
+                                           c_size_t, c_void_p]
+    lib.fc_decode_attention_ex.restype = c_int
     lib.fc_rotary.argtypes = [c_void_p, POINTER(fc_rotary_args), c_void_p]
     lib.fc_rotary.restype = c_int
     lib.fc_rotary_frequencies.argtypes = [c_int32, c_double, POINTER(fc_rope_scaling), POINTER(c_double), POINTER(c_double)]
@@ -544,6 +554,56 @@ def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
     _counter(used, "used", 1)
     _check(_lib.fc_dequantize_cache(handle, byref(cache.c), out_k.data_ptr(), out_v.data_ptr(), rows,
                                     used.data_ptr() if used is not None else None, _stream_of(out_k)), "fc_dequantize_cache")
+
+
+def make_decode_args_ex(q, cache, offsets, max_rows: int, tail_k=None, tail_v=None, tail_len=None, window: int = 0, sinks: int = 0):
+    """-> (arguments, options) of fc_decode_attention_ex.  cache: a Cache4, or (cache_k, cache_v) [rows, H, d]; window 0: every row
+    is visible, else the last `window` rows and the first `sinks`.  The rest as make_decode_args.  The arguments hold pointers:
+    keep the tensors."""
+    opt = fc_decode_options(window=int(window), sinks=int(sinks))
+    if isinstance(cache, Cache4):
+        B, Hq, d = (int(x) for x in q.shape)
+        if not q.is_contiguous() or q.dtype != cache.dtype:
+            raise ValueError("q: contiguous, of the cache's type")
+        a = fc_decode_args(q=q.data_ptr(), cache_rows=cache.capacity_rows, offsets=offsets.data_ptr(), dtype=_DTYPE[q.dtype], batch=B,
+                           num_heads=cache.num_heads, num_q_heads=Hq, head_dim=d, max_rows=int(max_rows))
+        opt.cache4 = ctypes.pointer(cache.c)
+        opt._kept = cache
+        H, kept = cache.num_heads, (cache.codes_k,)
+    else:
+        cache_k, cache_v = cache
+        a = make_decode_args(q, cache_k, cache_v, offsets, max_rows)
+        B, H, d, kept = int(q.shape[0]), int(cache_k.shape[1]), int(q.shape[2]), (cache_k, cache_v)
+        if cache_k.dim() != 3 or cache_v.shape != cache_k.shape or int(cache_k.shape[2]) != d:
+            raise ValueError("cache_k, cache_v: [rows, H, d]")
+    _counter(offsets, "offsets", B + 1)
+    if tail_k is not None:
+        if tail_v is None or tail_len is None or tail_len.dtype != torch.int32 or tuple(tail_len.shape) != (B,):
+            raise ValueError("tail_k with tail_v and tail_len, int32 [B]")
+        for t in (tail_k, tail_v):
+            if not t.is_contiguous() or t.dtype != q.dtype or t.shape != tail_k.shape or t.dim() != 4 or t.shape[0] != B \
+                    or tuple(t.shape[2:]) != (H, d):
+                raise ValueError("tail_k/tail_v: contiguous [B, cap, H, d] of the cache's type")
+        a.tail_k, a.tail_v, a.tail_len = tail_k.data_ptr(), tail_v.data_ptr(), tail_len.data_ptr()
+        a.tail_capacity = int(tail_k.shape[1])
+    _same_device(q, offsets, tail_k, tail_v, tail_len, *kept)
+    a._device = q
+    return a, opt
+
+
+def fc_decode_workspace_bytes_ex(handle, args, options) -> int:
+    n = int(_lib.fc_decode_workspace_bytes_ex(handle, byref(args), byref(options)))
+    if n == 0:
+        raise FlashCacheError(1, "fc_decode_workspace_bytes_ex")
+    return n
+
+
+def fc_decode_attention_ex(handle, args, options, out, workspace) -> None:
+    """out: [B, Hq, d] device tensor of the cache's type."""
+    rc = _lib.fc_decode_attention_ex(handle, byref(args), byref(options), out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                     _stream_of(args._device))
+    if rc != FC_OK:
+        raise FlashCacheError(rc, "fc_decode_attention_ex")
 
 
 ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}

@@ -16,12 +16,14 @@
 // Both launches are programmatic dependents: they are set up while the kernel before them in the stream ends.
 // Together: 28 layers of 65536 rows 965 -> 784 us per step, of those kept rows with tails 397 -> 310 us (from a graph 754
 // and 294; the host enqueues the 28 calls in 230..370 us, behind the device).
-#include <cuda.h>
-
 #include "fc_common.cuh"
+#include "fc_line.cuh"
 #include "fc_mbar.cuh"
+#include "fc_tile.cuh"
 
 namespace {
+
+using namespace tile;
 
 constexpr int kD = 128;                 // head_dim
 constexpr int kTile = 64;               // rows per tile
@@ -52,60 +54,6 @@ struct DecodeMaps {
   CUtensorMap k, v, tk, tv;
 };
 
-// Tiled loads into this block's shared memory; completion is counted in bytes on `bar`.  One destination block only.
-__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2,
-                                            unsigned long long *bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
-               ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(reinterpret_cast<unsigned long long>(map)),
-                 "r"(c0), "r"(c1), "r"(c2), "r"((unsigned)__cvta_generic_to_shared(bar)) : "memory");
-}
-__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, int c3,
-                                            unsigned long long *bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n"
-               ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(reinterpret_cast<unsigned long long>(map)),
-                 "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"((unsigned)__cvta_generic_to_shared(bar)) : "memory");
-}
-
-__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
-  asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<unsigned long long>(map)) : "memory");
-}
-
-__device__ __forceinline__ void ldmatrix_x4(unsigned addr, unsigned (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(unsigned addr, unsigned (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-
-// D += A (16x16, row) * B (16x8, col), fp32 accumulation.
-template <typename T> struct Mma;
-template <> struct Mma<__half> {
-  __device__ static void run(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  }
-  __device__ static unsigned pack(float x, float y) {
-    const __half2 h = __floats2half2_rn(x, y);
-    return *reinterpret_cast<const unsigned *>(&h);
-  }
-  __device__ static __half from_float(float x) { return __float2half_rn(x); }
-};
-template <> struct Mma<__nv_bfloat16> {
-  __device__ static void run(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  }
-  __device__ static unsigned pack(float x, float y) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    return *reinterpret_cast<const unsigned *>(&h);
-  }
-  __device__ static __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
-};
-
 // Byte offset of the 16-byte chunk `chunk` (0..15 over the 128 channels) of row `row` (0..63) inside a K or V
 // half-pair as the two swizzled TMA boxes leave it: channels 0..63 in the first box, 64..127 in the second;
 // inside a box a row is 128 bytes and chunk j of row r sits at position j ^ (r & 7).
@@ -134,59 +82,11 @@ __device__ __forceinline__ SeqRows seq_rows(const DecodeParams &P, int b) {
   return s;
 }
 
-// The line of T tiles, head after head and sequence after sequence: block i takes the tiles [i*T/nb, (i+1)*T/nb).
-// (32-bit division where the product fits: a 64-bit one costs some hundred cycles before the first load.)
-__device__ __forceinline__ long long muldiv(long long a, int m, long long d) {
-  const unsigned long long x = (unsigned long long)a * (unsigned)m;
-  return (x >> 32) == 0 && ((unsigned long long)d >> 32) == 0 ? (long long)((unsigned)x / (unsigned)d) : (long long)(x / (unsigned long long)d);
-}
-__device__ __forceinline__ long long share_start(int i, long long T, int nb) { return muldiv(T, i, nb); }
-__device__ __forceinline__ int share_of(long long t, long long T, int nb) {
-  const unsigned long long x = (unsigned long long)(t + 1) * (unsigned)nb - 1;
-  return (x >> 32) == 0 && ((unsigned long long)T >> 32) == 0 ? (int)((unsigned)x / (unsigned)T) : (int)(x / (unsigned long long)T);
-}
-
-// A block's share of the line: tiles [lo, hi), the first of them in sequence b of head h, whose tiles start at `line`.
-struct Share {
-  long long lo, hi, line, line_len;
-  int h, b, nb;                                // nb: blocks that have tiles
-};
-// Tiles of all sequences, 32 at a time, in every warp for itself (no barrier before the first load): the sum, then
-// the sequence that holds the first tile of this block's share.
+using line::Share;
+using line::share_of;
 template <bool EARLY>
 __device__ __forceinline__ Share find_share(const DecodeParams &P, int blk, int lane) {
-  Share r;
-  auto tiles_of = [&](int i) { return i < P.B ? seq_rows<EARLY>(P, i).tiles : 0; };
-  const int first32 = tiles_of(lane);
-  long long total = __reduce_add_sync(0xffffffffu, first32);
-  for (int b0 = 32; b0 < P.B; b0 += 32) total += __reduce_add_sync(0xffffffffu, tiles_of(b0 + lane));
-  r.line_len = total * P.H;                    // every head has the same tiles
-  r.nb = r.line_len < P.nb ? (int)r.line_len : P.nb;
-  r.lo = blk < r.nb ? share_start(blk, r.line_len, r.nb) : 0;
-  r.hi = blk < r.nb ? share_start(blk + 1, r.line_len, r.nb) : 0;
-  r.h = r.lo > 0 ? (int)muldiv(r.lo, 1, total) : 0;
-  const long long lo_head = r.lo - r.h * total;              // within the head
-  r.b = 0;
-  r.line = 0;
-  long long at = 0;
-  for (int b0 = 0; b0 < P.B; b0 += 32) {
-    const int mine = b0 == 0 ? first32 : tiles_of(b0 + lane);
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    const unsigned past = __ballot_sync(0xffffffffu, at + incl > lo_head);
-    if (past) {
-      const int first = __ffs(past) - 1;
-      r.b = b0 + first;
-      r.line = r.h * total + at + __shfl_sync(0xffffffffu, incl - mine, first);
-      break;
-    }
-    at += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  return r;
+  return line::find_share(P.B, P.H, P.nb, blk, lane, [&](int i) { return seq_rows<EARLY>(P, i).tiles; });
 }
 
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;\n" ::"n"(kConsumers) : "memory"); }
@@ -550,23 +450,6 @@ k_decode_combine(const DecodeParams P) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// Looked up once; a thread that comes while another one looks waits for it (handles of several threads may call at once).
-EncodeTiledFn encode_fn() {
-  static const EncodeTiledFn fn = [] {
-    void *p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-                   q == cudaDriverEntryPointSuccess
-               ? reinterpret_cast<EncodeTiledFn>(p)
-               : nullptr;
-  }();
-  return fn;
-}
-
 // Tiles of 64 rows x 64 channels of one head, rows 128 bytes wide in shared memory, 128-byte swizzle.
 fc_status encode_rows(CUtensorMap *m, CUtensorMapDataType dt, int rank, const void *base, const cuuint64_t *dims,
                       const cuuint64_t *strides_b) {

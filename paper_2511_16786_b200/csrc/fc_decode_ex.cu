@@ -1,0 +1,857 @@
+// Decoding step over rows held in 4 bits or in 16, with or without a window and sinks (fc_decode_attention_ex).
+//
+// For every sequence and query head  out = sum_j w_j v_j / sum_j w_j,  w_j = exp(q k_j / sqrt d)  over the visible rows j: kept
+// rows, then the 16-bit tail.  A step reads every visible row once and is bound by that read, so the frame is that of
+// fc_decode.cu: the tiles of all sequences and heads form one line, one block per SM takes an equal share of it, a warp
+// keeps a ring of tiles in flight, the other warps only ever wait for the tile they use, blocks that share a sequence meet
+// in a second kernel.  What differs:
+//
+//  * A row of 4 bits is 72 bytes of K or V at d = 128 instead of 256, so the arithmetic per byte is 3.6 times that of 16-bit
+//    rows and the instructions per row, not the bytes, are what could run out.  Nothing is expanded in memory or to fp32:
+//    - codes are masked out of the loaded words and are the tensor cores' operands as they stand, as subnormal half numbers
+//      (code * 2^-24, exact; the second nibble of a word is 16 times that, which the queries or the output rows undo);
+//    - a half row's scale multiplies sums of 32 products (keys) or the weights (values), never a code;
+//    - its minimum goes with the sum of the query's channels (keys) or with a sum of weights (values), both in fp32.
+//    Scores take queries as the products' rows; outputs are kept turned round, channels as rows and queries as columns, since
+//    the scores' accumulator is then the second product's operand in place, and eight columns are enough for 8 query heads.
+//  * Queries are brought to 2^14 .. 2^15 by a power of two before they become half numbers (exact but for channels 2^-25 of the
+//    largest); weights are kept below 2^15 together with the largest scale met so far, so rounding them to half numbers (11 bits)
+//    neither overflows nor loses the small ones, whatever the range of the cache's type.
+//  * Kept rows of 16 bits and tails come in tiles of 32 rows (two warps each, 16 KB at d = 128, about what 128 rows of 4 bits take),
+//    so every tile of the line costs about the same.
+//  * A window makes of a sequence's tiles the first few and the last ones; rows of them that are not visible get no weight.
+#include "fc_cache4.cuh"
+#include "fc_line.cuh"
+#include "fc_mbar.cuh"
+#include "fc_tile.cuh"
+
+namespace {
+
+using namespace tile;
+using line::Share;
+
+constexpr int kWarps = 8;                      // consumer warps; one more loads
+constexpr int kConsumers = 32 * kWarps;
+constexpr int kThreads = kConsumers + 32;
+constexpr int kRows4 = 16 * kWarps;            // rows of a 4-bit tile
+constexpr int kRows16 = 32;                    // rows of a 16-bit tile
+constexpr float kTop = 14.f, kReset = 10.f;    // weights times the largest scale: at most 2^kTop, 2^kReset after a move
+
+struct ExParams {
+  const void *q;
+  void *out;
+  const long long *offsets;
+  const int *tail_len;
+  float *part_o;                               // [slot][query heads of a KV head][D]
+  float2 *part_ml;                             // [slot][query heads of a KV head]: (reference, sum)
+  int2 *span;                                  // [H][batch]: first and last block with tiles of the sequence (first > last: none)
+  int *status;
+  int B, H, Hq, G, nb, tail_cap, has_tail, window, sinks;
+  float scale_log2;                            // log2(e) / sqrt(D)
+  long long cache_rows;
+  const unsigned char *ck, *cv, *pk, *pv;      // a 4-bit cache
+};
+
+struct ExMaps {
+  CUtensorMap k, v, tk, tv;                    // k, v: only of 16-bit rows
+};
+
+// A sequence's tiles: of the kept rows [0, a) and [b, c), then of the tail [ta, tb) and [tc, td) (tile numbers).
+struct SeqTiles {
+  long long off0, start;                       // first row; where its tiles start (even in a 4-bit cache: copies are in 16 bytes)
+  int n_main, n_tail;
+  int low, high;                               // visible: rows < low and rows >= high
+  int a, b, main, ta, tb, tiles;               // main: tiles of kept rows in the list; ta, tb as a, b
+};
+
+template <bool Q4>
+__device__ __forceinline__ SeqTiles seq_tiles(const ExParams &P, int i) {
+  constexpr int M = Q4 ? kRows4 : kRows16;
+  SeqTiles s;
+  long long r0 = P.offsets[i], r1 = P.offsets[i + 1];
+  r1 = r1 > P.cache_rows ? P.cache_rows : r1;  // rows that the cache does not have are none
+  r0 = r0 < 0 ? 0 : r0;
+  s.off0 = r0;
+  s.n_main = r1 > r0 ? (int)(r1 - r0) : 0;
+  const int nt = P.has_tail ? P.tail_len[i] : 0;
+  s.n_tail = nt < 0 ? 0 : (nt > P.tail_cap ? P.tail_cap : nt);
+  const int n = s.n_main + s.n_tail, skew = Q4 ? (int)(r0 & 1) : 0;
+  s.start = r0 - skew;
+  s.low = n;
+  s.high = n;
+  if (P.window > 0 && n > P.window && n - P.window > P.sinks) {
+    s.low = P.sinks;
+    s.high = n - P.window;
+  }
+  auto up = [](int x, int m) { return (x + m - 1) / m; };
+  const int all = s.n_main ? up(s.n_main + skew, M) : 0;
+  s.a = s.n_main ? up((s.low < s.n_main ? s.low : s.n_main) + (s.low ? skew : 0), M) : 0;
+  s.b = s.high < s.n_main ? (s.high + skew) / M : all;
+  s.b = s.b < s.a ? s.a : s.b;
+  s.main = s.a + all - s.b;
+  const int tall = up(s.n_tail, kRows16), tlow = s.low - s.n_main, thigh = s.high - s.n_main;
+  s.ta = up(tlow < 0 ? 0 : (tlow < s.n_tail ? tlow : s.n_tail), kRows16);
+  s.tb = (thigh < 0 ? 0 : (thigh < s.n_tail ? thigh : s.n_tail)) / kRows16;
+  if (thigh >= s.n_tail) s.tb = tall;
+  s.tb = s.tb < s.ta ? s.ta : s.tb;
+  s.tiles = s.main + s.ta + tall - s.tb;
+  return s;
+}
+// local tile lt -> is it of the tail, its number there, the row (of the sequence) it starts at
+struct TileAt {
+  bool tail;
+  int number, row;
+};
+template <bool Q4>
+__device__ __forceinline__ TileAt tile_at(const SeqTiles &s, int lt) {
+  TileAt t;
+  t.tail = lt >= s.main;
+  if (!t.tail) {
+    t.number = lt < s.a ? lt : lt - s.a + s.b;
+    t.row = t.number * (Q4 ? kRows4 : kRows16) - (Q4 ? (int)(s.off0 - s.start) : 0);
+  } else {
+    lt -= s.main;
+    t.number = lt < s.ta ? lt : lt - s.ta + s.tb;
+    t.row = s.n_main + t.number * kRows16;
+  }
+  return t;
+}
+
+__device__ __forceinline__ void load_bytes(void *dst, const void *src, unsigned bytes, unsigned long long *bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
+               ::"r"(mbar::address(dst)), "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(mbar::address(bar)) : "memory");
+}
+
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;\n" ::"n"(kConsumers) : "memory"); }
+
+// Sizes in shared memory.  A stage holds a 4-bit tile (codes of K, of V, parameters of K, of V) or a 16-bit one (K, V as boxes of 64 channels).
+template <int D, bool Q4, int NQ>
+struct Geo {
+  static constexpr int kCode = D / 2, kParam = cache4::kParamBytes;
+  static constexpr int kBytes4 = kRows4 * 2 * (kCode + kParam);
+  static constexpr int kBox = kRows16 * 128, kBytes16 = 2 * (D / 64) * kBox;
+  static constexpr int kStage = ((Q4 && kBytes4 > kBytes16 ? kBytes4 : kBytes16) + 1023) / 1024 * 1024;
+  static constexpr int kStride = D + 4;        // floats per row of a warp's output in the merge buffer
+  static constexpr int kMerge = kWarps * 8 * NQ * (kStride + 4) * (int)sizeof(float);    // output, (reference, sum), two sums of minima
+  static constexpr int kRoom = 226 * 1024 - 1024 - 256 - kMerge;
+  static constexpr int kStages = kRoom / kStage > 10 ? 10 : kRoom / kStage;
+  static constexpr size_t kSmem = (size_t)kStages * kStage + kMerge + 1024;
+};
+
+template <typename T> __device__ __forceinline__ float2 two(unsigned w);
+template <> __device__ __forceinline__ float2 two<__half>(unsigned w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+template <> __device__ __forceinline__ float2 two<__nv_bfloat16>(unsigned w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+template <typename T, int D, bool Q4, int NQ>
+__global__ void __launch_bounds__(kThreads)
+k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M) {
+  using S = Geo<D, Q4, NQ>;
+  constexpr int kStages = S::kStages, kHeads = 8 * NQ, MT = D / 16;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  float *mbuf = reinterpret_cast<float *>(smem + kStages * S::kStage);
+  __shared__ unsigned long long full[kStages], empty[kStages];
+  const int blk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar::init(&full[i], 1u); mbar::init(&empty[i], kWarps); }
+    mbar::init_done();
+  }
+  if (tid == kConsumers) {
+    if (!Q4) { prefetch_map(&M.k); prefetch_map(&M.v); }
+    if (P.has_tail) { prefetch_map(&M.tk); prefetch_map(&M.tv); }
+  }
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");       // what the kernels before this one wrote is visible from here
+
+  const Share sr = line::find_share(P.B, P.H, P.nb, blk, lane, [&](int i) { return seq_tiles<Q4>(P, i).tiles; });
+  const long long lo = sr.lo, hi = sr.hi, line_len = sr.line_len;
+  const int nb = sr.nb;
+  int h = sr.h, b = sr.b;
+  long long at = sr.line;
+  if (blk == 0)                                // sequences without rows
+    for (int i = tid; i < P.B; i += kThreads)
+      if (seq_tiles<Q4>(P, i).tiles == 0) {
+        for (int hh = 0; hh < P.H; ++hh) P.span[(size_t)hh * P.B + i] = make_int2(0, -1);
+        for (int c = 0; c < P.Hq * D / 8; ++c)
+          reinterpret_cast<uint4 *>(static_cast<T *>(P.out) + (size_t)i * P.Hq * D)[c] = make_uint4(0u, 0u, 0u, 0u);
+      }
+  if (lo >= hi) return;
+  SeqTiles s = seq_tiles<Q4>(P, b);
+  auto advance = [&](long long ti) {           // on to the sequence and head that tile ti belongs to
+    while (ti >= at + s.tiles) {
+      at += s.tiles;
+      if (++b == P.B) { b = 0; ++h; }
+      s = seq_tiles<Q4>(P, b);
+    }
+  };
+
+  if (warp == kWarps) {
+    // producer
+    if (lane == 0) {
+      int n = 0;
+      bool ok = true;
+      for (long long ti = lo; ti < hi; ++ti, ++n) {
+        advance(ti);
+        const int st = n % kStages;
+        if (n >= kStages && !mbar::wait(&empty[st], (unsigned)(n / kStages - 1) & 1u)) { ok = false; break; }
+        unsigned char *dst = smem + st * S::kStage;
+        const TileAt ta = tile_at<Q4>(s, (int)(ti - at));
+        if (Q4 && !ta.tail) {
+          const long long row = s.start + (long long)ta.number * kRows4;            // even, and even many: runs of 16 bytes
+          const long long end = s.off0 + s.n_main - row;
+          const unsigned rows = (unsigned)(end < kRows4 ? end + (end & 1) : kRows4);
+          mbar::expect_tx(&full[st], rows * 2u * (S::kCode + S::kParam));
+          const size_t r = (size_t)h * P.cache_rows + row;
+          load_bytes(dst, P.ck + r * S::kCode, rows * S::kCode, &full[st]);
+          load_bytes(dst + 2 * kRows4 * S::kCode, P.pk + r * S::kParam, rows * S::kParam, &full[st]);
+          load_bytes(dst + kRows4 * S::kCode, P.cv + r * S::kCode, rows * S::kCode, &full[st]);
+          load_bytes(dst + kRows4 * (2 * S::kCode + S::kParam), P.pv + r * S::kParam, rows * S::kParam, &full[st]);
+        } else {
+          mbar::expect_tx(&full[st], (unsigned)S::kBytes16);
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) {
+            if (!ta.tail) {
+              const int r = (int)(s.off0 + (long long)ta.number * kRows16);
+              tma_load_3d(dst + c * S::kBox, &M.k, 64 * c, h, r, &full[st]);
+              tma_load_3d(dst + (D / 64 + c) * S::kBox, &M.v, 64 * c, h, r, &full[st]);
+            } else {
+              tma_load_4d(dst + c * S::kBox, &M.tk, 64 * c, h, ta.number * kRows16, b, &full[st]);
+              tma_load_4d(dst + (D / 64 + c) * S::kBox, &M.tv, 64 * c, h, ta.number * kRows16, b, &full[st]);
+            }
+          }
+        }
+      }
+      if (!mbar::drain(full, n)) ok = false;   // no block ends under its own loads
+      if (!ok) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
+    }
+    return;
+  }
+
+  // consumers
+  const unsigned sbase = mbar::address(smem);
+  float *mo = mbuf;                                                        // [warp][kHeads][kStride]
+  float2 *mml = reinterpret_cast<float2 *>(mo + kWarps * kHeads * S::kStride);   // [warp][kHeads]
+  float2 *mmin = mml + kWarps * kHeads;                                    // [warp][kHeads]: weights times minima, either half
+  bool failed = false;
+  int n = 0;
+  for (long long ti = lo; ti < hi;) {
+    advance(ti);
+    const long long seg_end = at + s.tiles < hi ? at + s.tiles : hi;
+    const T *qb = static_cast<const T *>(P.q) + ((long long)b * P.Hq + (long long)h * P.G) * D;
+    // the query heads of this KV head as the 16-row operand, in the order of the tile's channels (rows past the group are zero)
+    unsigned qf[MT][2 * NQ];                   // NQ == 1: rows 8..15 are zero and have no registers
+    float qsum[NQ][2] = {}, qback[NQ] = {};    // of a 4-bit tile: log2(e)/sqrt(d) times the halves' sums; what undoes the power of two
+    auto load_q4 = [&]() {
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        const bool mine = g + 8 * r < P.G;
+        const T *row = qb + (g + 8 * r) * D;
+        float top = 0.f, sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {         // channels 16 i + 4 t ..
+          const uint2 w = mine ? *reinterpret_cast<const uint2 *>(row + 16 * i + 4 * t) : make_uint2(0u, 0u);
+          const float2 x = two<T>(w.x), y = two<T>(w.y);
+          top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+          sum[i / (MT / 2)] += (x.x + x.y) + (y.x + y.y);
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], o);
+          sum[1] += __shfl_xor_sync(0xffffffffu, sum[1], o);
+        }
+        int e = (int)(__float_as_uint(top) >> 23);                         // biased exponent of the largest
+        e = e < 16 ? 16 : (e > 254 ? 254 : e);
+        const float f = __uint_as_float((unsigned)(268 - e) << 23);        // 2^(14 - (e - 127))
+        // a sum of codes * 2^-24 times queries * f, times this: the score's part in log2 units
+        qback[r] = P.scale_log2 * 16777216.f * __uint_as_float((unsigned)(e - 14) << 23);
+        qsum[r][0] = sum[0] * P.scale_log2;
+        qsum[r][1] = sum[1] * P.scale_log2;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const uint2 w = mine ? *reinterpret_cast<const uint2 *>(row + 16 * i + 4 * t) : make_uint2(0u, 0u);
+          const float2 x = two<T>(w.x), y = two<T>(w.y);
+          qf[i][r] = Mma<__half>::pack(x.x * f, x.y * f);
+          qf[i][NQ + r] = Mma<__half>::pack(y.x * f * 0.0625f, y.y * f * 0.0625f);      // meets 16 times the code
+        }
+      }
+    };
+    auto load_q16 = [&]() {
+#pragma unroll
+      for (int r = 0; r < NQ; ++r)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const T *row = qb + (g + 8 * r) * D + 16 * i + 2 * t;
+          qf[i][r] = g + 8 * r < P.G ? *reinterpret_cast<const unsigned *>(row) : 0u;
+          qf[i][NQ + r] = g + 8 * r < P.G ? *reinterpret_cast<const unsigned *>(row + 8) : 0u;
+        }
+    };
+    // output: rows (channels) g and g + 8 of 16, columns (queries) 2t, 2t+1 of 8.  Beside 4-bit tiles rows g are in units of
+    // 2^-24 and rows g + 8 of 2^-20.
+    float oacc[MT][NQ][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
+    float omin[NQ][2] = {};                    // sums of weight * minimum over this lane's rows, for query g (+8)
+    float m[NQ], l[NQ] = {};                   // reference of the weights (log2) and their sum over this lane's rows, query g (+8)
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) m[r] = -INFINITY;
+    float vtop = 0.f, vexp = 0.f;              // a power of two that no value scale met so far passes, and its exponent (0: none yet)
+    bool in4 = false, have_q = false;
+    auto to_one = [&]() {                      // output from the units of 4-bit tiles to 1
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) {
+          oacc[i][r][0] *= 16777216.f; oacc[i][r][1] *= 16777216.f;
+          oacc[i][r][2] *= 1048576.f; oacc[i][r][3] *= 1048576.f;
+        }
+    };
+    // new scores of query g (+8 r), four per lane: moves the reference where they need it (all lanes together)
+    auto refer = [&](const float (&sc)[NQ][4], float above) {
+      float need[NQ];
+      bool move = false;
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        float x = fmaxf(fmaxf(sc[r][0], sc[r][1]), fmaxf(sc[r][2], sc[r][3]));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+        need[r] = x + above;
+        move |= need[r] > m[r] + kTop;
+      }
+      if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) {
+          const float to = need[r] > m[r] + kTop ? need[r] - kReset : m[r];
+          const float c = m[r] == to ? 1.f : exp2f(m[r] - to);
+          m[r] = to;
+          l[r] *= c;
+          omin[r][0] *= c;
+          omin[r][1] *= c;
+          const float c0 = __shfl_sync(0xffffffffu, c, 8 * t), c1 = __shfl_sync(0xffffffffu, c, 8 * t + 4);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            oacc[i][r][0] *= c0; oacc[i][r][1] *= c1;
+            oacc[i][r][2] *= c0; oacc[i][r][3] *= c1;
+          }
+        }
+      }
+    };
+
+    for (; ti < seg_end; ++ti, ++n) {
+      if (failed) continue;
+      const int st = n % kStages;
+      if (!mbar::wait_warp(&full[st], (unsigned)(n / kStages) & 1u)) {
+        // a load did not arrive in time (for any lane): say so and report an empty share
+        failed = true;
+        if (lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
+        continue;
+      }
+      const TileAt ta = tile_at<Q4>(s, (int)(ti - at));
+      const unsigned sb = sbase + (unsigned)(st * S::kStage);
+      const int end = ta.tail ? s.n_main + s.n_tail : s.n_main;
+      auto sees = [&](int row) { return row >= 0 && row < end && (row < s.low || row >= s.high); };
+      // 16 rows of the tile are this warp's
+      const int first = Q4 && !ta.tail ? 16 * warp : 16 * (warp & 1);
+      const bool mine = (Q4 && !ta.tail) || (warp >> 1) == (n & 3);
+      const int row0 = ta.row + first;
+      // any of them visible?
+      const bool some = mine && row0 < end && row0 + 15 >= 0 && (row0 < s.low || row0 + 15 >= s.high);
+      if (some) {
+        const bool whole = row0 >= 0 && row0 + 16 <= end && (row0 + 16 <= s.low || row0 >= s.high);
+        if (Q4 && !ta.tail) {
+          if constexpr (Q4) {
+            if (!in4 || !have_q) { load_q4(); in4 = have_q = true; }       // kept rows come before the tail: never back
+            // this lane's columns of the scores, and rows of the second product: 8 j + t and 8 j + 7 - t
+            const int c0 = first + t, c1 = first + 7 - t;
+            const unsigned char *tile_p = smem + st * S::kStage;
+            unsigned kp[2][2][2], vp[2][2][2];                             // [j][column][half]: (scale, minimum)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const int row = 8 * j + (c ? c1 : c0);
+                const uint2 a = *reinterpret_cast<const uint2 *>(tile_p + 2 * kRows4 * S::kCode + row * S::kParam);
+                const uint2 v = *reinterpret_cast<const uint2 *>(tile_p + kRows4 * (2 * S::kCode + S::kParam) + row * S::kParam);
+                kp[j][c][0] = a.x; kp[j][c][1] = a.y;
+                vp[j][c][0] = v.x; vp[j][c][1] = v.y;
+              }
+            float acc[2][2][4];                                            // [j][half]
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[j][0][e] = acc[j][1][e] = 0.f;
+              const int row = first + 8 * j + ((g & 1) ? 7 - (g >> 1) : (g >> 1));
+              unsigned w[D / 32];
+              if (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(tile_p + row * S::kCode + t * (D / 8));
+                w[0] = x.x; w[1] = x.y; w[D / 32 - 2] = x.z; w[D / 32 - 1] = x.w;
+              } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(tile_p + row * S::kCode + t * (D / 8));
+                w[0] = x.x; w[1] = x.y;
+              }
+#pragma unroll
+              for (int i = 0; i < D / 32; ++i) {
+                const int half = i / (D / 64);
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                  const unsigned x = o ? w[i] >> 8 : w[i];
+                  const int sl = 2 * i + o;
+                  const unsigned a[4] = {qf[sl][0], NQ == 2 ? qf[sl][NQ - 1] : 0u, qf[sl][NQ], NQ == 2 ? qf[sl][2 * NQ - 1] : 0u};
+                  Mma<__half>::run(acc[j][half], a, x & 0x000f000fu, x & 0x00f000f0u);
+                }
+              }
+            }
+            float sc[NQ][4], ks[2][2][2], vs[2][2][2], vm[2][2][2], es = 0.f;
+            bool vis[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                vis[j][c] = whole || sees(row0 - first + 8 * j + (c ? c1 : c0));
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                  const float2 kx = two<T>(kp[j][c][u]), vx = two<T>(vis[j][c] ? vp[j][c][u] : 0u);
+                  ks[j][c][u] = kx.x;
+                  vs[j][c][u] = vx.x;
+                  vm[j][c][u] = vx.y;
+                  es = fmaxf(es, vx.x);
+#pragma unroll
+                  for (int r = 0; r < NQ; ++r) {
+                    const float part = fmaf(ks[j][c][u] * acc[j][u][2 * r + c], qback[r], kx.y * qsum[r][u]);
+                    sc[r][2 * j + c] = u ? sc[r][2 * j + c] + part : part;
+                  }
+                }
+#pragma unroll
+                for (int r = 0; r < NQ; ++r) sc[r][2 * j + c] = vis[j][c] ? sc[r][2 * j + c] : -INFINITY;
+              }
+            if (__any_sync(0xffffffffu, es > vtop)) {                      // a larger scale than any before
+#pragma unroll
+              for (int o = 1; o < 32; o <<= 1) es = fmaxf(es, __shfl_xor_sync(0xffffffffu, es, o));
+              int e = (int)(__float_as_uint(es) >> 23) + 1;                // es < 2^(e - 127)
+              e = e < 87 ? 87 : (e > 254 ? 254 : e);                       // not below 2^-40: sums of weights stay finite
+              vtop = __uint_as_float((unsigned)e << 23);
+              vexp = (float)(e - 127);
+            }
+            refer(sc, vexp);
+            unsigned pw[NQ][2][2];                                         // [half][j]: weight * scale of two rows
+#pragma unroll
+            for (int r = 0; r < NQ; ++r) {
+              const float ref = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const float p0 = exp2f(sc[r][2 * j] - ref), p1 = exp2f(sc[r][2 * j + 1] - ref);
+                l[r] += p0 + p1;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                  pw[r][u][j] = Mma<__half>::pack(p0 * vs[j][0][u], p1 * vs[j][1][u]);
+                  omin[r][u] = fmaf(p0, vm[j][0][u], fmaf(p1, vm[j][1][u], omin[r][u]));
+                }
+              }
+            }
+            // values: run g of the lane's four rows; nibble n of a run is channel 8 n + g
+            const unsigned char *vt = tile_p + kRows4 * S::kCode + g * (D / 16);
+            unsigned w[2][2][D / 64];                                      // [j][column][word]
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const unsigned char *p = vt + (8 * j + (c ? c1 : c0)) * S::kCode;
+                if (D == 128) {
+                  const uint2 x = *reinterpret_cast<const uint2 *>(p);
+                  w[j][c][0] = x.x; w[j][c][D / 64 - 1] = x.y;
+                } else {
+                  w[j][c][0] = *reinterpret_cast<const unsigned *>(p);
+                }
+              }
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+              for (int hw = 0; hw < 2; ++hw) {                             // nibbles 0..3, 4..7 of the word, of two rows side by side
+                unsigned x = __byte_perm(w[0][0][i], w[0][1][i], hw ? 0x7632 : 0x5410);
+                unsigned y = __byte_perm(w[1][0][i], w[1][1][i], hw ? 0x7632 : 0x5410);
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                  const int mt = 4 * i + 2 * hw + o, u = mt / (MT / 2);
+                  const unsigned a[4] = {x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u};
+#pragma unroll
+                  for (int r = 0; r < NQ; ++r) Mma<__half>::run(oacc[mt][r], a, pw[r][u][0], pw[r][u][1]);
+                  x >>= 8;
+                  y >>= 8;
+                }
+              }
+          }
+        } else {
+          if (in4) { to_one(); in4 = false; have_q = false; }
+          if (!have_q) { load_q16(); have_q = true; }
+          float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+          const int mi = lane >> 3;
+          // 16-byte chunk c of row r, as the swizzled boxes of 64 channels leave it
+          auto chunk_at = [&](int r, int c) { return (unsigned)((c >> 3) * S::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4)); };
+#pragma unroll
+          for (int kk = 0; kk < MT; ++kk) {
+            unsigned r[4];
+            ldmatrix_x4(sb + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * kk + (mi & 1)), r);
+            const unsigned a[4] = {qf[kk][0], NQ == 2 ? qf[kk][NQ - 1] : 0u, qf[kk][NQ], NQ == 2 ? qf[kk][2 * NQ - 1] : 0u};
+            Mma<T>::run(acc[0], a, r[0], r[1]);
+            Mma<T>::run(acc[1], a, r[2], r[3]);
+          }
+          float sc[NQ][4];
+          unsigned keep[2] = {0xffffffffu, 0xffffffffu};                   // bits of the rows 2t, 2t+1 (+ 8) that have weight
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const bool vis = whole || sees(row0 + 8 * j + 2 * t + c);
+              if (!vis) keep[j] &= c ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+              for (int r = 0; r < NQ; ++r) sc[r][2 * j + c] = vis ? acc[j][2 * r + c] * P.scale_log2 : -INFINITY;
+            }
+          refer(sc, 0.f);
+          unsigned pw[NQ][2];
+#pragma unroll
+          for (int r = 0; r < NQ; ++r) {
+            const float ref = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float p0 = exp2f(sc[r][2 * j] - ref), p1 = exp2f(sc[r][2 * j + 1] - ref);
+              l[r] += p0 + p1;
+              pw[r][j] = Mma<T>::pack(p0, p1);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            unsigned r[4];
+            ldmatrix_x4_trans(sb + (D / 64) * S::kBox + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * i + (mi & 1)), r);
+            // rows without weight may hold anything, and 0 x NaN is NaN
+            const unsigned a[4] = {r[0] & keep[0], r[1] & keep[0], r[2] & keep[1], r[3] & keep[1]};
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) Mma<T>::run(oacc[i][q], a, pw[q][0], pw[q][1]);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar::arrive(&empty[st]);                             // this warp is through with the stage
+    }
+    if (in4) to_one();
+    if (failed) {
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) { m[r] = -INFINITY; l[r] = 0.f; omin[r][0] = omin[r][1] = 0.f; }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
+    }
+
+    // merge the warps
+    consumers_sync();                                                      // the merge buffer is free again
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) {
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+        omin[r][0] += __shfl_xor_sync(0xffffffffu, omin[r][0], o);
+        omin[r][1] += __shfl_xor_sync(0xffffffffu, omin[r][1], o);
+      }
+      float *w = mo + ((size_t)warp * kHeads + 8 * r) * S::kStride;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        w[(2 * t) * S::kStride + 16 * i + g] = oacc[i][r][0];
+        w[(2 * t + 1) * S::kStride + 16 * i + g] = oacc[i][r][1];
+        w[(2 * t) * S::kStride + 16 * i + 8 + g] = oacc[i][r][2];
+        w[(2 * t + 1) * S::kStride + 16 * i + 8 + g] = oacc[i][r][3];
+      }
+      if (t == 0) {
+        mml[warp * kHeads + 8 * r + g] = make_float2(m[r], l[r]);
+        mmin[warp * kHeads + 8 * r + g] = make_float2(omin[r][0], omin[r][1]);
+      }
+    }
+    consumers_sync();
+    const int i0 = line::share_of(at, line_len, nb), i1 = line::share_of(at + s.tiles - 1, line_len, nb);
+    const size_t slot = ((size_t)blk + (size_t)h * P.B + b) * P.G;
+    constexpr int C = D / 32;                                              // channels per lane
+    for (int r = warp; r < P.G; r += kWarps) {                             // a warp per query head
+      float2 ml[kWarps];
+      float mm = -INFINITY, ll = 0.f, o[C];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) { ml[w] = mml[w * kHeads + r]; mm = fmaxf(mm, ml[w].x); }
+      const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2f(ml[w].x - ref);
+        const float *src = mo + ((size_t)w * kHeads + r) * S::kStride + C * lane;
+        const float2 mn = mmin[w * kHeads + r];
+        const float add = lane < 16 ? mn.x : mn.y;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = fmaf(src[c] + add, f, o[c]);
+        ll = fmaf(ml[w].y, f, ll);
+      }
+      if (i0 == i1) {
+        const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);    // a NaN sum stays one
+        T *out = static_cast<T *>(P.out) + ((size_t)b * P.Hq + (size_t)h * P.G + r) * D + C * lane;
+#pragma unroll
+        for (int c = 0; c < C; c += 2) *reinterpret_cast<unsigned *>(out + c) = Mma<T>::pack(o[c] * inv, o[c + 1] * inv);
+      } else {
+        float *dst = P.part_o + (slot + r) * D + C * lane;
+#pragma unroll
+        for (int c = 0; c < C; c += 2) *reinterpret_cast<float2 *>(dst + c) = make_float2(o[c], o[c + 1]);
+        if (lane == 0) P.part_ml[slot + r] = make_float2(mm, ll);
+      }
+    }
+    if (blk == i0 && tid == 0) P.span[(size_t)h * P.B + b] = make_int2(i0, i1);
+  }
+}
+
+// out of a sequence that several blocks share: their results rescaled to the common reference and divided by the common sum.
+// Block i's result of sequence (h, b) is in slot i + h*B + b (both only ever advance along the line, so slots do not collide).
+template <typename T, int D>
+__global__ void __launch_bounds__(128)
+k_decode_ex_combine(const __grid_constant__ ExParams P) {
+  constexpr int C = D / 32, kFold = 4, kAhead = 8;
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  __shared__ float so[kFold][D];
+  __shared__ float2 sml[kFold];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int b = blockIdx.x / P.Hq, hq = blockIdx.x - b * P.Hq, h = hq / P.G, r = hq - h * P.G;
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int2 span = __ldcg(P.span + (size_t)h * P.B + b);
+  if (span.y <= span.x) return;                                            // no rows, or finished by its only block
+  const size_t slot0 = ((size_t)span.x + (size_t)h * P.B + b) * P.G + r;
+  const int cnt = span.y - span.x + 1;
+  float acc[C], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) acc[c] = 0.f;
+  for (int s0 = warp; s0 < cnt; s0 += kFold * kAhead) {
+    float v[kAhead][C];
+    float2 ml[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int i = s0 + a * kFold < cnt ? s0 + a * kFold : s0;
+      ml[a] = __ldcg(P.part_ml + slot0 + (size_t)i * P.G);
+#pragma unroll
+      for (int c = 0; c < C; c += 2) {
+        const float2 x = __ldcg(reinterpret_cast<const float2 *>(P.part_o + (slot0 + (size_t)i * P.G) * D + C * lane + c));
+        v[a][c] = x.x; v[a][c + 1] = x.y;
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      if (s0 + a * kFold >= cnt) ml[a] = make_float2(-INFINITY, 0.f);
+      mn = fmaxf(mn, ml[a].x);
+    }
+    const float ref = mn == -INFINITY ? 0.f : mn, keep = exp2f(m - ref);
+    m = mn;
+    l *= keep;
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] *= keep;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      if (s0 + a * kFold < cnt) {
+        const float f = exp2f(ml[a].x - ref);
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] = fmaf(v[a][c], f, acc[c]);
+        l = fmaf(ml[a].y, f, l);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) so[warp][C * lane + c] = acc[c];
+  if (lane == 0) sml[warp] = make_float2(m, l);
+  __syncthreads();
+  if (warp != 0) return;
+  float mm = -INFINITY, ll = 0.f, o[C];
+#pragma unroll
+  for (int w = 0; w < kFold; ++w) mm = fmaxf(mm, sml[w].x);
+  const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+  for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kFold; ++w) {
+    const float f = exp2f(sml[w].x - ref);
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = fmaf(so[w][C * lane + c], f, o[c]);
+    ll = fmaf(sml[w].y, f, ll);
+  }
+  const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
+  T *out = static_cast<T *>(P.out) + ((size_t)b * P.Hq + hq) * D + C * lane;
+#pragma unroll
+  for (int c = 0; c < C; c += 2) *reinterpret_cast<unsigned *>(out + c) = Mma<T>::pack(o[c] * inv, o[c + 1] * inv);
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+// Tiles of 32 rows x 64 channels of one head, rows 128 bytes wide in shared memory, 128-byte swizzle.
+fc_status encode_rows(CUtensorMap *m, CUtensorMapDataType dt, int rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return FC_ERR_CUDA;
+  const cuuint32_t box[4] = {64, 1, (cuuint32_t)kRows16, 1}, ones[4] = {1, 1, 1, 1};
+  return fn(m, dt, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? FC_OK : FC_ERR_INTERNAL;
+}
+
+fc_status check_ex(const fc_handle *h, const fc_decode_args *a, const fc_decode_options *o) {
+  if (!h || !a || !o || !a->q || !a->offsets) return FC_ERR_INVALID_ARG;
+  if (a->batch < 1 || a->num_heads < 1 || a->num_q_heads < 1 || a->max_rows < 0 || o->window < 0 || o->sinks < 0) return FC_ERR_INVALID_ARG;
+  if (a->dtype != FC_F16 && a->dtype != FC_BF16) return FC_ERR_UNSUPPORTED;
+  if (a->head_dim != 64 && a->head_dim != 128) return FC_ERR_UNSUPPORTED;
+  if (a->num_q_heads % a->num_heads != 0 || a->num_q_heads / a->num_heads > 16) return FC_ERR_UNSUPPORTED;
+  if (o->cache4) {
+    const fc_status s = cache4::check(o->cache4);
+    if (s != FC_OK) return s;
+    if (o->cache4->dtype != a->dtype || o->cache4->num_heads != a->num_heads || o->cache4->head_dim != a->head_dim) return FC_ERR_INVALID_ARG;
+  } else {
+    if (!a->cache_k || !a->cache_v || a->cache_rows < 1) return FC_ERR_INVALID_ARG;
+    if (((uintptr_t)a->cache_k & 15) || ((uintptr_t)a->cache_v & 15)) return FC_ERR_INVALID_ARG;
+    if (a->cache_rows > 0x7fffffffll - 4096) return FC_ERR_UNSUPPORTED;
+  }
+  if (a->max_rows > 0x7fffffffll - 4096 || a->batch > 65535 || a->num_heads > 65535 ||
+      (int64_t)a->batch * a->num_q_heads > 0x7fffffffll)
+    return FC_ERR_UNSUPPORTED;
+  if ((uintptr_t)a->q & 15) return FC_ERR_INVALID_ARG;
+  if (a->tail_k || a->tail_v || a->tail_len) {
+    if (!a->tail_k || !a->tail_v || !a->tail_len || a->tail_capacity < 1) return FC_ERR_INVALID_ARG;
+    if (((uintptr_t)a->tail_k & 15) || ((uintptr_t)a->tail_v & 15)) return FC_ERR_INVALID_ARG;
+    if (a->tail_capacity > 0x7fffffff - 4096) return FC_ERR_UNSUPPORTED;
+  }
+  return FC_OK;
+}
+
+struct ExPlan {
+  int nb;
+  size_t off_ml, off_span, total;
+};
+
+ExPlan plan_ex(const fc_handle *h, const fc_decode_args *a, const fc_decode_options *o) {
+  ExPlan p;
+  // one block per SM (the ring takes most of its shared memory), or as many as there can be tiles: of what a sequence of
+  // max_rows rows shows, however it splits into kept rows, tail, sinks and window (each part's ends may cut a tile)
+  const long long size = o->cache4 ? kRows4 : kRows16;
+  long long rows = a->max_rows;
+  if (o->window > 0 && (long long)o->window + o->sinks < rows) rows = (long long)o->window + o->sinks;
+  const long long per = (rows + size - 1) / size + 3 + (a->tail_k ? (a->tail_capacity < rows ? a->tail_capacity : rows) / kRows16 + 3 : 0);
+  const long long units = (long long)a->batch * a->num_heads, tiles = units * per;
+  p.nb = (int)(tiles < h->num_sms ? tiles : h->num_sms);
+  const size_t slots = (size_t)(p.nb + units) * (size_t)(a->num_q_heads / a->num_heads);
+  p.off_ml = (slots * a->head_dim * sizeof(float) + 255) & ~(size_t)255;
+  p.off_span = p.off_ml + ((slots * sizeof(float2) + 255) & ~(size_t)255);
+  p.total = p.off_span + (((size_t)units * sizeof(int2) + 255) & ~(size_t)255);
+  return p;
+}
+
+template <typename T, int D, bool Q4, int NQ>
+fc_status launch_ex(fc_handle *h, const ExParams &P, const ExMaps &M, cudaStream_t st) {
+  using S = Geo<D, Q4, NQ>;
+  static_assert(S::kStages >= 4 && S::kSmem <= 227 * 1024 - 512, "shared memory");
+  constexpr unsigned bit = 1u << ((std::is_same<T, __half>::value ? 1 : 0) + (D == 128 ? 2 : 0) + (Q4 ? 4 : 0) + (NQ == 2 ? 8 : 0));
+  if (!(h->decode_ex_ready & bit)) {           // once per handle
+    FC_CUDA_TRY(cudaFuncSetAttribute(k_decode_ex<T, D, Q4, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
+    h->decode_ex_ready |= bit;
+  }
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3(P.nb);
+  lc.blockDim = dim3(kThreads);
+  lc.dynamicSmemBytes = S::kSmem;
+  lc.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  if (cudaLaunchKernelEx(&lc, k_decode_ex<T, D, Q4, NQ>, P, M) != cudaSuccess) {
+    cudaGetLastError();
+    return FC_ERR_CUDA;
+  }
+  fc_status s = fc_after_launch(h);
+  if (s != FC_OK) return s;
+  lc.gridDim = dim3((unsigned)(P.B * P.Hq));
+  lc.blockDim = dim3(128);
+  lc.dynamicSmemBytes = 0;
+  if (cudaLaunchKernelEx(&lc, k_decode_ex_combine<T, D>, P) != cudaSuccess) {
+    cudaGetLastError();
+    return FC_ERR_CUDA;
+  }
+  return fc_after_launch(h);
+}
+
+template <typename T, int D>
+fc_status launch_of(fc_handle *h, const ExParams &P, const ExMaps &M, bool q4, cudaStream_t st) {
+  if (q4) return P.G <= 8 ? launch_ex<T, D, true, 1>(h, P, M, st) : launch_ex<T, D, true, 2>(h, P, M, st);
+  return P.G <= 8 ? launch_ex<T, D, false, 1>(h, P, M, st) : launch_ex<T, D, false, 2>(h, P, M, st);
+}
+
+}  // namespace
+
+extern "C" size_t fc_decode_workspace_bytes_ex(const fc_handle *h, const fc_decode_args *a, const fc_decode_options *opt) {
+  if (!opt) return fc_decode_workspace_bytes(h, a);
+  if (check_ex(h, a, opt) != FC_OK) return 0;
+  return plan_ex(h, a, opt).total;
+}
+
+extern "C" fc_status fc_decode_attention_ex(fc_handle *h, const fc_decode_args *a, const fc_decode_options *opt, void *out,
+                                            void *workspace, size_t workspace_bytes, fc_stream stream) {
+  if (!opt) return fc_decode_attention(h, a, out, workspace, workspace_bytes, stream);
+  fc_status s = check_ex(h, a, opt);
+  if (s != FC_OK) return s;
+  if (!out || ((uintptr_t)out & 15)) return FC_ERR_INVALID_ARG;
+  const ExPlan pl = plan_ex(h, a, opt);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pl.total) return FC_ERR_WORKSPACE;
+  FcDeviceGuard on(h->device);
+  if (!on.ok) return FC_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if ((s = fc_flush_pending(h, st)) != FC_OK) return s;
+  const int D = a->head_dim;
+  const CUtensorMapDataType dt = a->dtype == FC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const cuuint64_t head_b = (cuuint64_t)D * 2, row_b = (cuuint64_t)a->num_heads * head_b;
+  ExMaps M = {};
+  if (!opt->cache4) {
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a->num_heads, (cuuint64_t)a->cache_rows}, str[2] = {head_b, row_b};
+    if ((s = encode_rows(&M.k, dt, 3, a->cache_k, dims, str)) != FC_OK) return s;
+    if ((s = encode_rows(&M.v, dt, 3, a->cache_v, dims, str)) != FC_OK) return s;
+  }
+  if (a->tail_k) {
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)a->num_heads, (cuuint64_t)a->tail_capacity, (cuuint64_t)a->batch};
+    const cuuint64_t str[3] = {head_b, row_b, row_b * (cuuint64_t)a->tail_capacity};
+    if ((s = encode_rows(&M.tk, dt, 4, a->tail_k, dims, str)) != FC_OK) return s;
+    if ((s = encode_rows(&M.tv, dt, 4, a->tail_v, dims, str)) != FC_OK) return s;
+  }
+  char *ws = static_cast<char *>(workspace);
+  ExParams P = {};
+  P.q = a->q;
+  P.out = out;
+  P.offsets = reinterpret_cast<const long long *>(a->offsets);
+  P.tail_len = a->tail_len;
+  P.part_o = reinterpret_cast<float *>(ws);
+  P.part_ml = reinterpret_cast<float2 *>(ws + pl.off_ml);
+  P.span = reinterpret_cast<int2 *>(ws + pl.off_span);
+  P.status = h->status_word;
+  P.B = a->batch;
+  P.H = a->num_heads;
+  P.Hq = a->num_q_heads;
+  P.G = a->num_q_heads / a->num_heads;
+  P.nb = pl.nb;
+  P.tail_cap = a->tail_k ? a->tail_capacity : 0;
+  P.has_tail = a->tail_k ? 1 : 0;
+  P.window = opt->window;
+  P.sinks = opt->sinks;
+  P.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
+  P.cache_rows = opt->cache4 ? opt->cache4->capacity_rows : a->cache_rows;
+  if (opt->cache4) {
+    P.ck = static_cast<const unsigned char *>(opt->cache4->codes_k);
+    P.cv = static_cast<const unsigned char *>(opt->cache4->codes_v);
+    P.pk = static_cast<const unsigned char *>(opt->cache4->params_k);
+    P.pv = static_cast<const unsigned char *>(opt->cache4->params_v);
+  }
+  const bool q4 = opt->cache4 != nullptr;
+  if (a->dtype == FC_F16) return D == 128 ? launch_of<__half, 128>(h, P, M, q4, st) : launch_of<__half, 64>(h, P, M, q4, st);
+  return D == 128 ? launch_of<__nv_bfloat16, 128>(h, P, M, q4, st) : launch_of<__nv_bfloat16, 64>(h, P, M, q4, st);
+}
