@@ -418,6 +418,37 @@ fc_status fc_decode_attention_ex(fc_handle *h, const fc_decode_args *a, const fc
                                  void *workspace, size_t workspace_bytes, fc_stream stream);
 
 /*
+ * Attention of a prefill, or of a chunk of one, with a sliding window and sinks: for every sequence b with n_q queries and
+ * n_k keys, query i stands at position p = n_k - n_q + i and
+ *     out[i] = Softmax over visible j (q[i] k[j] / sqrt(head_dim)) v[j],   j visible:  j <= p and (j > p - window or j < sinks).
+ * window >= n_k: plain causal attention.  A query that sees no key (p < 0) gives zeros.  fp32 scores, statistics and sums;
+ * weights are rounded to dtype before the second product.  A key or value that is not finite reaches the queries that see
+ * it and no other.
+ *
+ *   q            DEVICE [Tq][num_q_heads][head_dim] with strides (elements, channel stride 1, 16-byte aligned)
+ *   kv           keys and values: FC_F16 or FC_BF16, head_dim 64 or 128; query head j reads KV head j / (num_q_heads / num_heads)
+ *   cu_seqlens_q HOST int32[kv->batch + 1], like kv->cu_seqlens, which counts the keys
+ *   window >= 1, sinks >= 0
+ *   out          DEVICE dense [Tq][num_q_heads][head_dim]
+ *   workspace    DEVICE, 256-byte aligned, >= fc_window_workspace_bytes() (where few queries face many keys, the keys are
+ *                split over blocks whose results meet there)
+ * Limits: num_q_heads a multiple of num_heads, at most 64 query heads per KV head.
+ * Errors: FC_ERR_INVALID_ARG, FC_ERR_UNSUPPORTED, FC_ERR_WORKSPACE, FC_ERR_CUDA; a bounded wait that runs out sets
+ * FC_ERR_TIMEOUT in the device status word.
+ */
+typedef struct {
+  const void *q;
+  int64_t q_stride_token, q_stride_head;
+  int32_t num_q_heads, window, sinks;
+  const int32_t *cu_seqlens_q;
+  const fc_kv_view *kv;
+} fc_window_args;
+
+size_t fc_window_workspace_bytes(const fc_handle *h, const fc_window_args *a);
+fc_status fc_window_attention(fc_handle *h, const fc_window_args *a, void *out, void *workspace, size_t workspace_bytes,
+                              fc_stream stream);
+
+/*
  * Rotary positions.  The first rotary_dim channels of a head are rotary_dim/2 pairs, (j, j + rotary_dim/2) or, interleaved,
  * (2j, 2j+1); pair j of a token at position p turns by p * freq[j]:
  *     (a, b) -> (a c - b s, b c + a s),  c = scale*cos, s = scale*sin  (inverse: s = -scale*sin; with scale 1 this undoes

@@ -30,7 +30,7 @@ EXPORTS = (
     "fc_select_compact_layers", "fc_layer_capacity_rows", "fc_score_layers", "fc_score_layers_workspace_bytes",
     "fc_power_spectrum_workspace_bytes", "fc_power_spectrum", "fc_cutoff_from_spectrum",
     "fc_decode_workspace_bytes", "fc_decode_attention",
-    "fc_decode_workspace_bytes_ex", "fc_decode_attention_ex",
+    "fc_decode_workspace_bytes_ex", "fc_decode_attention_ex", "fc_window_workspace_bytes", "fc_window_attention",
     "fc_quantize_cache", "fc_dequantize_cache", "fc_rotary", "fc_rotary_frequencies",
     "fc_static_scratch_bytes", "fc_score_layer_static", "fc_static_last_device_status",
     "fc_compress_host_rows", "fc_compress_host_arena_bytes", "fc_compress_host",
@@ -71,6 +71,11 @@ class fc_cache4(ctypes.Structure):
 
 class fc_decode_options(ctypes.Structure):
     _fields_ = [("cache4", POINTER(fc_cache4)), ("window", c_int32), ("sinks", c_int32)]
+
+
+class fc_window_args(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("q_stride_token", c_int64), ("q_stride_head", c_int64), ("num_q_heads", c_int32), ("window", c_int32),
+                ("sinks", c_int32), ("cu_seqlens_q", POINTER(c_int32)), ("kv", POINTER(fc_kv_view))]
 
 
 class fc_rotary_args(ctypes.Structure):
@@ -208,6 +213,10 @@ def _load() -> ctypes.CDLL:
     lib.fc_decode_attention_ex.argtypes = [c_void_p, POINTER(fc_decode_args), POINTER(fc_decode_options), c_void_p, c_void_p,
                                            c_size_t, c_void_p]
     lib.fc_decode_attention_ex.restype = c_int
+    lib.fc_window_workspace_bytes.argtypes = [c_void_p, POINTER(fc_window_args)]
+    lib.fc_window_workspace_bytes.restype = c_size_t
+    lib.fc_window_attention.argtypes = [c_void_p, POINTER(fc_window_args), c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.fc_window_attention.restype = c_int
     lib.fc_rotary.argtypes = [c_void_p, POINTER(fc_rotary_args), c_void_p]
     lib.fc_rotary.restype = c_int
     lib.fc_rotary_frequencies.argtypes = [c_int32, c_double, POINTER(fc_rope_scaling), POINTER(c_double), POINTER(c_double)]
@@ -604,6 +613,41 @@ def fc_decode_attention_ex(handle, args, options, out, workspace) -> None:
                                      _stream_of(args._device))
     if rc != FC_OK:
         raise FlashCacheError(rc, "fc_decode_attention_ex")
+
+
+def make_window_args(q, k, v, cu_seqlens_q, cu_seqlens_k, window: int, sinks: int = 0):
+    """q: [Tq, Hq, d]; k, v: [Tk, H, d]; cumulated lengths of queries and of keys, on the host.  The arguments hold pointers: keep
+    the tensors."""
+    cq, ck = _cu_array(cu_seqlens_q), _cu_array(cu_seqlens_k)
+    view = make_view(k, v, ck)
+    if q.dim() != 3 or q.stride(2) != 1 or q.dtype != k.dtype or q.shape[2] != k.shape[2] or len(cq) != len(ck):
+        raise ValueError("q: [Tq, Hq, d] of the keys' type with channel stride 1; lengths of as many sequences")
+    if q.shape[0] < cq[len(cq) - 1] or k.shape[0] < ck[len(ck) - 1]:
+        raise ValueError("more tokens in the lengths than in the tensors")
+    _same_device(q, k, v)
+    # strides of single heads and tokens may be anything in a tensor
+    view.stride_head = k.stride(1) if k.shape[1] > 1 else k.shape[2]
+    view.stride_token = k.stride(0) if k.shape[0] > 1 else k.shape[1] * k.shape[2]
+    a = fc_window_args(q=q.data_ptr(), q_stride_token=q.stride(0) if q.shape[0] > 1 else q.shape[1] * q.shape[2],
+                       q_stride_head=q.stride(1) if q.shape[1] > 1 else q.shape[2], num_q_heads=int(q.shape[1]), window=int(window),
+                       sinks=int(sinks), cu_seqlens_q=ctypes.cast(cq, POINTER(c_int32)), kv=ctypes.pointer(view))
+    a._kept = (cq, ck, view)
+    a._device = q
+    return a
+
+
+def fc_window_workspace_bytes(handle, args) -> int:
+    n = int(_lib.fc_window_workspace_bytes(handle, byref(args)))
+    if n == 0:
+        raise FlashCacheError(1, "fc_window_workspace_bytes")
+    return n
+
+
+def fc_window_attention(handle, args, out, workspace) -> None:
+    """out: contiguous [Tq, Hq, d] of q's type."""
+    rc = _lib.fc_window_attention(handle, byref(args), out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(args._device))
+    if rc != FC_OK:
+        raise FlashCacheError(rc, "fc_window_attention")
 
 
 ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}

@@ -153,7 +153,7 @@ extern "C" fc_status fc_create(fc_handle **out, int device, int32_t max_seqlen) 
   h->done_counter = nullptr;
   h->small_counter = nullptr;
   h->decode_ready = false;
-  h->decode_ex_ready = 0;
+  h->forms_ready = 0;
   h->group_bytes = (size_t)32 << 20;
   h->launches = 0;
   h->num_aux = 2;

@@ -39,7 +39,7 @@ struct fc_handle {
   int *status_word;        // DEVICE
   unsigned *done_counter;  // DEVICE [2][FC_LAYER_CHUNK] pass 3, [1] allocation; zero between calls (the last block resets its counter)
   bool decode_ready;       // the decoding kernel has been allowed its shared memory on this device
-  unsigned decode_ex_ready;  // the same of the forms of fc_decode_attention_ex, a bit each
+  unsigned forms_ready;    // the same of the forms of fc_decode_attention_ex and fc_window_attention, a bit each
   unsigned *small_counter; // DEVICE [FC_LAYER_CHUNK * 32], zero between launches (fc_score_small.cuh)
   size_t group_bytes;
   int num_sms;

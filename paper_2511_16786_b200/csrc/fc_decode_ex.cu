@@ -753,9 +753,9 @@ fc_status launch_ex(fc_handle *h, const ExParams &P, const ExMaps &M, cudaStream
   using S = Geo<D, Q4, NQ>;
   static_assert(S::kStages >= 4 && S::kSmem <= 227 * 1024 - 512, "shared memory");
   constexpr unsigned bit = 1u << ((std::is_same<T, __half>::value ? 1 : 0) + (D == 128 ? 2 : 0) + (Q4 ? 4 : 0) + (NQ == 2 ? 8 : 0));
-  if (!(h->decode_ex_ready & bit)) {           // once per handle
+  if (!(h->forms_ready & bit)) {           // once per handle
     FC_CUDA_TRY(cudaFuncSetAttribute(k_decode_ex<T, D, Q4, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
-    h->decode_ex_ready |= bit;
+    h->forms_ready |= bit;
   }
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3(P.nb);
