@@ -31,9 +31,10 @@ using namespace tile;
 using line::Share;
 
 constexpr int kWarps = 8;                      // consumer warps; one more loads
+constexpr int kTeam = 4;                       // of them on one tile: two teams take the tiles of a block by turns
 constexpr int kConsumers = 32 * kWarps;
 constexpr int kThreads = kConsumers + 32;
-constexpr int kRows4 = 16 * kWarps;            // rows of a 4-bit tile
+constexpr int kRows4 = 32 * kTeam;             // rows of a 4-bit tile
 constexpr int kRows16 = 32;                    // rows of a 16-bit tile
 constexpr float kTop = 14.f, kReset = 10.f;    // weights times the largest scale: at most 2^kTop, 2^kReset after a move
 
@@ -134,9 +135,15 @@ struct Geo {
   static constexpr int kStride = D + 4;        // floats per row of a warp's output in the merge buffer
   static constexpr int kMerge = kWarps * 8 * NQ * (kStride + 4) * (int)sizeof(float);    // output, (reference, sum), two sums of minima
   static constexpr int kRoom = 226 * 1024 - 1024 - 256 - kMerge;
-  static constexpr int kStages = kRoom / kStage > 10 ? 10 : kRoom / kStage;
+  static constexpr int kStages = (kRoom / kStage > 10 ? 10 : kRoom / kStage) & ~1;       // even: a stage is always the same team's
   static constexpr size_t kSmem = (size_t)kStages * kStage + kMerge + 1024;
 };
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 template <typename T> __device__ __forceinline__ float2 two(unsigned w);
 template <> __device__ __forceinline__ float2 two<__half>(unsigned w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
@@ -153,11 +160,12 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float *mbuf = reinterpret_cast<float *>(smem + kStages * S::kStage);
   __shared__ unsigned long long full[kStages], empty[kStages];
-  const int blk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int blk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
+  const int team = warp / kTeam;
 
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar::init(&full[i], 1u); mbar::init(&empty[i], kWarps); }
+    for (int i = 0; i < kStages; ++i) { mbar::init(&full[i], 1u); mbar::init(&empty[i], kTeam); }
     mbar::init_done();
   }
   if (tid == kConsumers) {
@@ -297,8 +305,9 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
-    float omin[NQ][2] = {};                    // sums of weight * minimum over this lane's rows, for query g (+8)
-    float m[NQ], l[NQ] = {};                   // reference of the weights (log2) and their sum over this lane's rows, query g (+8)
+    float2 omin[NQ][2] = {};                   // sums of weight * minimum over this lane's rows (two columns), for query g (+8)
+    float m[NQ];                               // reference of the weights (log2), query g (+8)
+    float2 l[NQ] = {};                         // their sum
 #pragma unroll
     for (int r = 0; r < NQ; ++r) m[r] = -INFINITY;
     float vtop = 0.f, vexp = 0.f;              // a power of two that no value scale met so far passes, and its exponent (0: none yet)
@@ -312,27 +321,20 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
           oacc[i][r][2] *= 1048576.f; oacc[i][r][3] *= 1048576.f;
         }
     };
-    // new scores of query g (+8 r), four per lane: moves the reference where they need it (all lanes together)
-    auto refer = [&](const float (&sc)[NQ][4], float above) {
-      float need[NQ];
+    // the largest of new scores of query g (+8 r) asks for a reference (all lanes together)
+    auto refer = [&](const float (&x)[NQ], float above) {
       bool move = false;
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) {
-        float x = fmaxf(fmaxf(sc[r][0], sc[r][1]), fmaxf(sc[r][2], sc[r][3]));
-        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-        need[r] = x + above;
-        move |= need[r] > m[r] + kTop;
-      }
+      for (int r = 0; r < NQ; ++r) move |= x[r] + above > m[r] + kTop;
       if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
         for (int r = 0; r < NQ; ++r) {
-          const float to = need[r] > m[r] + kTop ? need[r] - kReset : m[r];
+          const float need = x[r] + above, to = need > m[r] + kTop ? need - kReset : m[r];
           const float c = m[r] == to ? 1.f : exp2f(m[r] - to);
           m[r] = to;
-          l[r] *= c;
-          omin[r][0] *= c;
-          omin[r][1] *= c;
+          l[r].x *= c; l[r].y *= c;
+          omin[r][0].x *= c; omin[r][0].y *= c;
+          omin[r][1].x *= c; omin[r][1].y *= c;
           const float c0 = __shfl_sync(0xffffffffu, c, 8 * t), c1 = __shfl_sync(0xffffffffu, c, 8 * t + 4);
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
@@ -342,206 +344,233 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         }
       }
     };
+    auto over_lanes = [&](float x) {                                       // the lanes of a query
+      x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+      return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+    };
+    // 32 rows of a 4-bit tile from `row0` of the sequence on; `first`: their place in the tile.  WHOLE: all are visible.
+    auto rows4 = [&](const unsigned char *tile_p, int first, int row0, int end, auto whole) {
+      constexpr bool WHOLE = decltype(whole)::value;
+      auto sees = [&](int row) { return row >= 0 && row < end && (row < s.low || row >= s.high); };
+      float2 sc[NQ][4];                                                    // [16 rows, 8 rows]: the lane's two columns of 8
+      float2 vs[4][2], vm[4][2];                                           // their value scales and minima, [half]
+      float es = 0.f, top[NQ];
+#pragma unroll
+      for (int b8 = 0; b8 < 4; ++b8) {                                     // 8 rows: columns t and 7 - t are this lane's
+        const int base = first + 8 * b8;
+        uint2 kp[2], vp[2];                                                // (scale, minimum) of either half
+        float acc[2][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[0][e] = acc[1][e] = 0.f;
+        unsigned w[D / 32];
+        const unsigned char *codes = tile_p + (base + ((g & 1) ? 7 - (g >> 1) : (g >> 1))) * S::kCode + t * (D / 8);
+        if (D == 128) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(codes);
+          w[0] = x.x; w[1] = x.y; w[D / 32 - 2] = x.z; w[D / 32 - 1] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2 *>(codes);
+          w[0] = x.x; w[1] = x.y;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const unsigned char *par = tile_p + 2 * kRows4 * S::kCode + (base + (c ? 7 - t : t)) * S::kParam;
+          kp[c] = *reinterpret_cast<const uint2 *>(par);
+          vp[c] = *reinterpret_cast<const uint2 *>(par + kRows4 * S::kParam);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+#pragma unroll
+          for (int o = 0; o < 2; ++o) {
+            const unsigned x = o ? w[i] >> 8 : w[i];
+            const int sl = 2 * i + o;
+            const unsigned a[4] = {qf[sl][0], NQ == 2 ? qf[sl][NQ - 1] : 0u, qf[sl][NQ], NQ == 2 ? qf[sl][2 * NQ - 1] : 0u};
+            Mma<__half>::run(acc[i / (D / 64)], a, x & 0x000f000fu, x & 0x00f000f0u);
+          }
+        }
+        bool vis[2] = {true, true};
+        if (!WHOLE) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            vis[c] = sees(row0 + 8 * b8 + (c ? 7 - t : t));
+            if (!vis[c]) vp[c] = make_uint2(0u, 0u);
+          }
+        }
+        const float2 k00 = two<T>(kp[0].x), k01 = two<T>(kp[0].y), k10 = two<T>(kp[1].x), k11 = two<T>(kp[1].y);
+        const float2 v00 = two<T>(vp[0].x), v01 = two<T>(vp[0].y), v10 = two<T>(vp[1].x), v11 = two<T>(vp[1].y);
+        vs[b8][0] = make_float2(v00.x, v10.x); vm[b8][0] = make_float2(v00.y, v10.y);
+        vs[b8][1] = make_float2(v01.x, v11.x); vm[b8][1] = make_float2(v01.y, v11.y);
+        es = fmaxf(fmaxf(es, fmaxf(v00.x, v01.x)), fmaxf(v10.x, v11.x));
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) {
+          float2 part = __fmul2_rn(make_float2(k00.x, k10.x), make_float2(acc[0][2 * r], acc[0][2 * r + 1]));
+          part = __ffma2_rn(make_float2(k01.x, k11.x), make_float2(acc[1][2 * r], acc[1][2 * r + 1]), part);
+          float2 low = __fmul2_rn(make_float2(k00.y, k10.y), make_float2(qsum[r][0], qsum[r][0]));
+          low = __ffma2_rn(make_float2(k01.y, k11.y), make_float2(qsum[r][1], qsum[r][1]), low);
+          float2 x = __ffma2_rn(part, make_float2(qback[r], qback[r]), low);
+          if (!WHOLE) {
+            x.x = vis[0] ? x.x : -INFINITY;
+            x.y = vis[1] ? x.y : -INFINITY;
+          }
+          sc[r][b8] = x;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < NQ; ++r)
+        top[r] = over_lanes(fmaxf(fmaxf(fmaxf(sc[r][0].x, sc[r][0].y), fmaxf(sc[r][1].x, sc[r][1].y)),
+                                  fmaxf(fmaxf(sc[r][2].x, sc[r][2].y), fmaxf(sc[r][3].x, sc[r][3].y))));
+      if (__any_sync(0xffffffffu, es > vtop)) {                            // a larger scale than any before
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) es = fmaxf(es, __shfl_xor_sync(0xffffffffu, es, o));
+        int e = (int)(__float_as_uint(es) >> 23) + 1;                      // es < 2^(e - 127)
+        e = e < 87 ? 87 : (e > 254 ? 254 : e);                             // not below 2^-40: sums of weights stay finite
+        vtop = __uint_as_float((unsigned)e << 23);
+        vexp = (float)(e - 127);
+      }
+      refer(top, vexp);
+      unsigned pw[NQ][2][4];                                               // [half][8 rows]: weight * scale of two rows
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+        for (int b8 = 0; b8 < 4; ++b8) {
+          const float2 x = __fadd2_rn(sc[r][b8], make_float2(-ref, -ref));
+          const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          l[r] = __fadd2_rn(l[r], p);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float2 y = __fmul2_rn(p, vs[b8][u]);
+            pw[r][u][b8] = Mma<__half>::pack(y.x, y.y);
+            omin[r][u] = __ffma2_rn(p, vm[b8][u], omin[r][u]);
+          }
+        }
+      }
+      // values: run g of the lane's rows; nibble n of a run is channel 8 n + g
+      const unsigned char *vt = tile_p + kRows4 * S::kCode + first * S::kCode + g * (D / 16);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        unsigned w[2][2][D / 64];                                          // [8 rows][column][word]
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const unsigned char *p = vt + (16 * jj + 8 * j + (c ? 7 - t : t)) * S::kCode;
+            if (D == 128) {
+              const uint2 x = *reinterpret_cast<const uint2 *>(p);
+              w[j][c][0] = x.x; w[j][c][D / 64 - 1] = x.y;
+            } else {
+              w[j][c][0] = *reinterpret_cast<const unsigned *>(p);
+            }
+          }
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+          for (int hw = 0; hw < 2; ++hw) {                                 // nibbles 0..3, 4..7 of the word, of two rows side by side
+            unsigned x = __byte_perm(w[0][0][i], w[0][1][i], hw ? 0x7632 : 0x5410);
+            unsigned y = __byte_perm(w[1][0][i], w[1][1][i], hw ? 0x7632 : 0x5410);
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+              const int mt = 4 * i + 2 * hw + o, u = mt / (MT / 2);
+              const unsigned a[4] = {x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u};
+#pragma unroll
+              for (int r = 0; r < NQ; ++r) Mma<__half>::run(oacc[mt][r], a, pw[r][u][2 * jj], pw[r][u][2 * jj + 1]);
+              x >>= 8;
+              y >>= 8;
+            }
+          }
+      }
+    };
+    // 16 rows of a 16-bit tile
+    auto rows16 = [&](unsigned sb, int first, int row0, int end) {
+      const bool whole = row0 >= 0 && row0 + 16 <= end && (row0 + 16 <= s.low || row0 >= s.high);
+      auto sees = [&](int row) { return row < end && (row < s.low || row >= s.high); };
+      float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      const int mi = lane >> 3;
+      // 16-byte chunk c of row r, as the swizzled boxes of 64 channels leave it
+      auto chunk_at = [&](int r, int c) { return (unsigned)((c >> 3) * S::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4)); };
+#pragma unroll
+      for (int kk = 0; kk < MT; ++kk) {
+        unsigned r[4];
+        ldmatrix_x4(sb + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * kk + (mi & 1)), r);
+        const unsigned a[4] = {qf[kk][0], NQ == 2 ? qf[kk][NQ - 1] : 0u, qf[kk][NQ], NQ == 2 ? qf[kk][2 * NQ - 1] : 0u};
+        Mma<T>::run(acc[0], a, r[0], r[1]);
+        Mma<T>::run(acc[1], a, r[2], r[3]);
+      }
+      float sc[NQ][4], top[NQ];
+      unsigned keep[2] = {0xffffffffu, 0xffffffffu};                       // bits of the rows 2t, 2t+1 (+ 8) that have weight
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const bool vis = whole || sees(row0 + 8 * j + 2 * t + c);
+          if (!vis) keep[j] &= c ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+          for (int r = 0; r < NQ; ++r) sc[r][2 * j + c] = vis ? acc[j][2 * r + c] * P.scale_log2 : -INFINITY;
+        }
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) top[r] = over_lanes(fmaxf(fmaxf(sc[r][0], sc[r][1]), fmaxf(sc[r][2], sc[r][3])));
+      refer(top, 0.f);
+      unsigned pw[NQ][2];
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float p0 = exp2_fast(sc[r][2 * j] - ref), p1 = exp2_fast(sc[r][2 * j + 1] - ref);
+          l[r].x += p0;
+          l[r].y += p1;
+          pw[r][j] = Mma<T>::pack(p0, p1);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        unsigned r[4];
+        ldmatrix_x4_trans(sb + (D / 64) * S::kBox + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * i + (mi & 1)), r);
+        // rows without weight may hold anything, and 0 x NaN is NaN
+        const unsigned a[4] = {r[0] & keep[0], r[1] & keep[0], r[2] & keep[1], r[3] & keep[1]};
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) Mma<T>::run(oacc[i][q], a, pw[q][0], pw[q][1]);
+      }
+    };
 
-    for (; ti < seg_end; ++ti, ++n) {
-      if (failed) continue;
-      const int st = n % kStages;
-      if (!mbar::wait_warp(&full[st], (unsigned)(n / kStages) & 1u)) {
+    const int lt0 = (int)(ti - at), cnt = (int)(seg_end - ti);
+    for (int i = (n ^ team) & 1; i < cnt && !failed; i += 2) {             // every second tile is this team's
+      const int st = (n + i) % kStages;
+      if (!mbar::wait_warp(&full[st], (unsigned)((n + i) / kStages) & 1u)) {
         // a load did not arrive in time (for any lane): say so and report an empty share
         failed = true;
         if (lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
-        continue;
+        break;
       }
-      const TileAt ta = tile_at<Q4>(s, (int)(ti - at));
-      const unsigned sb = sbase + (unsigned)(st * S::kStage);
+      const TileAt ta = tile_at<Q4>(s, lt0 + i);
       const int end = ta.tail ? s.n_main + s.n_tail : s.n_main;
-      auto sees = [&](int row) { return row >= 0 && row < end && (row < s.low || row >= s.high); };
-      // 16 rows of the tile are this warp's
-      const int first = Q4 && !ta.tail ? 16 * warp : 16 * (warp & 1);
-      const bool mine = (Q4 && !ta.tail) || (warp >> 1) == (n & 3);
-      const int row0 = ta.row + first;
-      // any of them visible?
-      const bool some = mine && row0 < end && row0 + 15 >= 0 && (row0 < s.low || row0 + 15 >= s.high);
-      if (some) {
-        const bool whole = row0 >= 0 && row0 + 16 <= end && (row0 + 16 <= s.low || row0 >= s.high);
-        if (Q4 && !ta.tail) {
-          if constexpr (Q4) {
-            if (!in4 || !have_q) { load_q4(); in4 = have_q = true; }       // kept rows come before the tail: never back
-            // this lane's columns of the scores, and rows of the second product: 8 j + t and 8 j + 7 - t
-            const int c0 = first + t, c1 = first + 7 - t;
+      if (Q4 && !ta.tail) {
+        if constexpr (Q4) {
+          const int first = 32 * (warp % kTeam), row0 = ta.row + first;
+          if (row0 < end && row0 + 31 >= 0 && (row0 < s.low || row0 + 31 >= s.high)) {
+            if (!in4) { load_q4(); in4 = true; }                           // kept rows come before the tail: never back
             const unsigned char *tile_p = smem + st * S::kStage;
-            unsigned kp[2][2][2], vp[2][2][2];                             // [j][column][half]: (scale, minimum)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const int row = 8 * j + (c ? c1 : c0);
-                const uint2 a = *reinterpret_cast<const uint2 *>(tile_p + 2 * kRows4 * S::kCode + row * S::kParam);
-                const uint2 v = *reinterpret_cast<const uint2 *>(tile_p + kRows4 * (2 * S::kCode + S::kParam) + row * S::kParam);
-                kp[j][c][0] = a.x; kp[j][c][1] = a.y;
-                vp[j][c][0] = v.x; vp[j][c][1] = v.y;
-              }
-            float acc[2][2][4];                                            // [j][half]
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[j][0][e] = acc[j][1][e] = 0.f;
-              const int row = first + 8 * j + ((g & 1) ? 7 - (g >> 1) : (g >> 1));
-              unsigned w[D / 32];
-              if (D == 128) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(tile_p + row * S::kCode + t * (D / 8));
-                w[0] = x.x; w[1] = x.y; w[D / 32 - 2] = x.z; w[D / 32 - 1] = x.w;
-              } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(tile_p + row * S::kCode + t * (D / 8));
-                w[0] = x.x; w[1] = x.y;
-              }
-#pragma unroll
-              for (int i = 0; i < D / 32; ++i) {
-                const int half = i / (D / 64);
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                  const unsigned x = o ? w[i] >> 8 : w[i];
-                  const int sl = 2 * i + o;
-                  const unsigned a[4] = {qf[sl][0], NQ == 2 ? qf[sl][NQ - 1] : 0u, qf[sl][NQ], NQ == 2 ? qf[sl][2 * NQ - 1] : 0u};
-                  Mma<__half>::run(acc[j][half], a, x & 0x000f000fu, x & 0x00f000f0u);
-                }
-              }
-            }
-            float sc[NQ][4], ks[2][2][2], vs[2][2][2], vm[2][2][2], es = 0.f;
-            bool vis[2][2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                vis[j][c] = whole || sees(row0 - first + 8 * j + (c ? c1 : c0));
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                  const float2 kx = two<T>(kp[j][c][u]), vx = two<T>(vis[j][c] ? vp[j][c][u] : 0u);
-                  ks[j][c][u] = kx.x;
-                  vs[j][c][u] = vx.x;
-                  vm[j][c][u] = vx.y;
-                  es = fmaxf(es, vx.x);
-#pragma unroll
-                  for (int r = 0; r < NQ; ++r) {
-                    const float part = fmaf(ks[j][c][u] * acc[j][u][2 * r + c], qback[r], kx.y * qsum[r][u]);
-                    sc[r][2 * j + c] = u ? sc[r][2 * j + c] + part : part;
-                  }
-                }
-#pragma unroll
-                for (int r = 0; r < NQ; ++r) sc[r][2 * j + c] = vis[j][c] ? sc[r][2 * j + c] : -INFINITY;
-              }
-            if (__any_sync(0xffffffffu, es > vtop)) {                      // a larger scale than any before
-#pragma unroll
-              for (int o = 1; o < 32; o <<= 1) es = fmaxf(es, __shfl_xor_sync(0xffffffffu, es, o));
-              int e = (int)(__float_as_uint(es) >> 23) + 1;                // es < 2^(e - 127)
-              e = e < 87 ? 87 : (e > 254 ? 254 : e);                       // not below 2^-40: sums of weights stay finite
-              vtop = __uint_as_float((unsigned)e << 23);
-              vexp = (float)(e - 127);
-            }
-            refer(sc, vexp);
-            unsigned pw[NQ][2][2];                                         // [half][j]: weight * scale of two rows
-#pragma unroll
-            for (int r = 0; r < NQ; ++r) {
-              const float ref = m[r] == -INFINITY ? 0.f : m[r];
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const float p0 = exp2f(sc[r][2 * j] - ref), p1 = exp2f(sc[r][2 * j + 1] - ref);
-                l[r] += p0 + p1;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                  pw[r][u][j] = Mma<__half>::pack(p0 * vs[j][0][u], p1 * vs[j][1][u]);
-                  omin[r][u] = fmaf(p0, vm[j][0][u], fmaf(p1, vm[j][1][u], omin[r][u]));
-                }
-              }
-            }
-            // values: run g of the lane's four rows; nibble n of a run is channel 8 n + g
-            const unsigned char *vt = tile_p + kRows4 * S::kCode + g * (D / 16);
-            unsigned w[2][2][D / 64];                                      // [j][column][word]
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const unsigned char *p = vt + (8 * j + (c ? c1 : c0)) * S::kCode;
-                if (D == 128) {
-                  const uint2 x = *reinterpret_cast<const uint2 *>(p);
-                  w[j][c][0] = x.x; w[j][c][D / 64 - 1] = x.y;
-                } else {
-                  w[j][c][0] = *reinterpret_cast<const unsigned *>(p);
-                }
-              }
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i)
-#pragma unroll
-              for (int hw = 0; hw < 2; ++hw) {                             // nibbles 0..3, 4..7 of the word, of two rows side by side
-                unsigned x = __byte_perm(w[0][0][i], w[0][1][i], hw ? 0x7632 : 0x5410);
-                unsigned y = __byte_perm(w[1][0][i], w[1][1][i], hw ? 0x7632 : 0x5410);
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                  const int mt = 4 * i + 2 * hw + o, u = mt / (MT / 2);
-                  const unsigned a[4] = {x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u};
-#pragma unroll
-                  for (int r = 0; r < NQ; ++r) Mma<__half>::run(oacc[mt][r], a, pw[r][u][0], pw[r][u][1]);
-                  x >>= 8;
-                  y >>= 8;
-                }
-              }
+            if (row0 >= 0 && row0 + 32 <= end && (row0 + 32 <= s.low || row0 >= s.high)) rows4(tile_p, first, row0, end, std::true_type{});
+            else rows4(tile_p, first, row0, end, std::false_type{});
           }
-        } else {
-          if (in4) { to_one(); in4 = false; have_q = false; }
-          if (!have_q) { load_q16(); have_q = true; }
-          float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-          const int mi = lane >> 3;
-          // 16-byte chunk c of row r, as the swizzled boxes of 64 channels leave it
-          auto chunk_at = [&](int r, int c) { return (unsigned)((c >> 3) * S::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4)); };
-#pragma unroll
-          for (int kk = 0; kk < MT; ++kk) {
-            unsigned r[4];
-            ldmatrix_x4(sb + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * kk + (mi & 1)), r);
-            const unsigned a[4] = {qf[kk][0], NQ == 2 ? qf[kk][NQ - 1] : 0u, qf[kk][NQ], NQ == 2 ? qf[kk][2 * NQ - 1] : 0u};
-            Mma<T>::run(acc[0], a, r[0], r[1]);
-            Mma<T>::run(acc[1], a, r[2], r[3]);
-          }
-          float sc[NQ][4];
-          unsigned keep[2] = {0xffffffffu, 0xffffffffu};                   // bits of the rows 2t, 2t+1 (+ 8) that have weight
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const bool vis = whole || sees(row0 + 8 * j + 2 * t + c);
-              if (!vis) keep[j] &= c ? 0x0000ffffu : 0xffff0000u;
-#pragma unroll
-              for (int r = 0; r < NQ; ++r) sc[r][2 * j + c] = vis ? acc[j][2 * r + c] * P.scale_log2 : -INFINITY;
-            }
-          refer(sc, 0.f);
-          unsigned pw[NQ][2];
-#pragma unroll
-          for (int r = 0; r < NQ; ++r) {
-            const float ref = m[r] == -INFINITY ? 0.f : m[r];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float p0 = exp2f(sc[r][2 * j] - ref), p1 = exp2f(sc[r][2 * j + 1] - ref);
-              l[r] += p0 + p1;
-              pw[r][j] = Mma<T>::pack(p0, p1);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            unsigned r[4];
-            ldmatrix_x4_trans(sb + (D / 64) * S::kBox + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * i + (mi & 1)), r);
-            // rows without weight may hold anything, and 0 x NaN is NaN
-            const unsigned a[4] = {r[0] & keep[0], r[1] & keep[0], r[2] & keep[1], r[3] & keep[1]};
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) Mma<T>::run(oacc[i][q], a, pw[q][0], pw[q][1]);
-          }
+        }
+      } else {
+        // two of the team's four warps, the others on its next tile
+        const int first = 16 * (warp & 1), row0 = ta.row + first;
+        if ((((warp % kTeam) >> 1) == (((n + i) >> 1) & 1)) && row0 < end && (row0 < s.low || row0 + 15 >= s.high)) {
+          if (in4 || !have_q) { load_q16(); have_q = true; }
+          if (in4) { to_one(); in4 = false; }
+          rows16(sbase + (unsigned)(st * S::kStage), first, row0, end);
         }
       }
       __syncwarp();
       if (lane == 0) mbar::arrive(&empty[st]);                             // this warp is through with the stage
     }
+    n += cnt;
+    ti = seg_end;
     if (in4) to_one();
     if (failed) {
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) { m[r] = -INFINITY; l[r] = 0.f; omin[r][0] = omin[r][1] = 0.f; }
+      for (int r = 0; r < NQ; ++r) { m[r] = -INFINITY; l[r] = omin[r][0] = omin[r][1] = make_float2(0.f, 0.f); }
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -552,11 +581,12 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     consumers_sync();                                                      // the merge buffer is free again
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
+      float lsum = l[r].x + l[r].y, min0 = omin[r][0].x + omin[r][0].y, min1 = omin[r][1].x + omin[r][1].y;
 #pragma unroll
       for (int o = 1; o < 4; o <<= 1) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
-        omin[r][0] += __shfl_xor_sync(0xffffffffu, omin[r][0], o);
-        omin[r][1] += __shfl_xor_sync(0xffffffffu, omin[r][1], o);
+        lsum += __shfl_xor_sync(0xffffffffu, lsum, o);
+        min0 += __shfl_xor_sync(0xffffffffu, min0, o);
+        min1 += __shfl_xor_sync(0xffffffffu, min1, o);
       }
       float *w = mo + ((size_t)warp * kHeads + 8 * r) * S::kStride;
 #pragma unroll
@@ -567,8 +597,8 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         w[(2 * t + 1) * S::kStride + 16 * i + 8 + g] = oacc[i][r][3];
       }
       if (t == 0) {
-        mml[warp * kHeads + 8 * r + g] = make_float2(m[r], l[r]);
-        mmin[warp * kHeads + 8 * r + g] = make_float2(omin[r][0], omin[r][1]);
+        mml[warp * kHeads + 8 * r + g] = make_float2(m[r], lsum);
+        mmin[warp * kHeads + 8 * r + g] = make_float2(min0, min1);
       }
     }
     consumers_sync();
