@@ -30,10 +30,13 @@ namespace {
 using namespace tile;
 using line::Share;
 
-constexpr int kWarps = 8;                      // consumer warps; one more loads
-constexpr int kTeam = 4;                       // of them on one tile: two teams take the tiles of a block by turns
+constexpr int kTeam = 4;                       // warps on one tile
+constexpr int kTeams = 3;                      // that take the tiles of a block by turns
+constexpr int kWarps = kTeam * kTeams;         // consumer warps; the first of four more loads
 constexpr int kConsumers = 32 * kWarps;
-constexpr int kThreads = kConsumers + 32;
+constexpr int kThreads = kConsumers + 128;
+constexpr int kRegsLoad = 32, kRegsRows = 160; // registers of a thread: 128 at launch, moved from the loading warps to the others
+static_assert(kRegsLoad + kTeams * kRegsRows <= 128 * (kTeams + 1), "a register split has to come out of what was launched");
 constexpr int kRows4 = 32 * kTeam;             // rows of a 4-bit tile
 constexpr int kRows16 = 32;                    // rows of a 16-bit tile
 constexpr float kTop = 14.f, kReset = 10.f;    // weights times the largest scale: at most 2^kTop, 2^kReset after a move
@@ -135,9 +138,45 @@ struct Geo {
   static constexpr int kStride = D + 4;        // floats per row of a warp's output in the merge buffer
   static constexpr int kMerge = kWarps * 8 * NQ * (kStride + 4) * (int)sizeof(float);    // output, (reference, sum), two sums of minima
   static constexpr int kRoom = 226 * 1024 - 1024 - 256 - kMerge;
-  static constexpr int kStages = (kRoom / kStage > 10 ? 10 : kRoom / kStage) & ~1;       // even: a stage is always the same team's
+  static constexpr int kFit = kRoom / kStage > 12 ? 12 : kRoom / kStage;
+  static constexpr int kStages = kFit / kTeams * kTeams;                               // a stage is always the same team's
   static constexpr size_t kSmem = (size_t)kStages * kStage + kMerge + 1024;
 };
+
+// The first product of a sum: nothing is there yet.
+template <typename T>
+__device__ __forceinline__ void mma_first(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+  if (std::is_same<T, __half>::value)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+// An 8 x 8 block of 16-bit numbers, a row over four lanes, turned round.
+__device__ __forceinline__ unsigned transposed(unsigned x) {
+  unsigned y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+// Shared memory by its own address: one register, offsets in the instruction.
+__device__ __forceinline__ uint4 lds128(unsigned a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(unsigned a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ unsigned lds32(unsigned a) {
+  unsigned v;
+  asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(v) : "r"(a));
+  return v;
+}
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -152,7 +191,7 @@ template <> __device__ __forceinline__ float2 two<__nv_bfloat16>(unsigned w) {
 }
 
 template <typename T, int D, bool Q4, int NQ>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 1)
 k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M) {
   using S = Geo<D, Q4, NQ>;
   constexpr int kStages = S::kStages, kHeads = 8 * NQ, MT = D / 16;
@@ -197,9 +236,10 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     }
   };
 
-  if (warp == kWarps) {
+  if (warp >= kWarps) {
     // producer
-    if (lane == 0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsLoad));
+    if (warp == kWarps && lane == 0) {
       int n = 0;
       bool ok = true;
       for (long long ti = lo; ti < hi; ++ti, ++n) {
@@ -240,19 +280,24 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
   }
 
   // consumers
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsRows));
   const unsigned sbase = mbar::address(smem);
   float *mo = mbuf;                                                        // [warp][kHeads][kStride]
   float2 *mml = reinterpret_cast<float2 *>(mo + kWarps * kHeads * S::kStride);   // [warp][kHeads]
   float2 *mmin = mml + kWarps * kHeads;                                    // [warp][kHeads]: weights times minima, either half
+  // a number that lanes (g, .) have for query g, as that of the queries 2t and 2t + 1
+  auto of_columns = [&](float x) { return make_float2(__shfl_sync(0xffffffffu, x, 8 * t), __shfl_sync(0xffffffffu, x, 8 * t + 4)); };
   bool failed = false;
   int n = 0;
   for (long long ti = lo; ti < hi;) {
     advance(ti);
     const long long seg_end = at + s.tiles < hi ? at + s.tiles : hi;
     const T *qb = static_cast<const T *>(P.q) + ((long long)b * P.Hq + (long long)h * P.G) * D;
-    // the query heads of this KV head as the 16-row operand, in the order of the tile's channels (rows past the group are zero)
-    unsigned qf[MT][2 * NQ];                   // NQ == 1: rows 8..15 are zero and have no registers
-    float qsum[NQ][2] = {}, qback[NQ] = {};    // of a 4-bit tile: log2(e)/sqrt(d) times the halves' sums; what undoes the power of two
+    // The query heads of this KV head as columns of the right operand: query g (+ 8 r), depth as the left operand's channels.
+    // Scores then have rows (of the cache) as rows and queries as columns, like the output has channels and queries: what a lane
+    // keeps of a query (reference, sums) is of its columns 2t, 2t+1 (+ 8 r) throughout.
+    unsigned qf[MT][NQ][2];
+    float2 qsum[NQ][2] = {}, qback[NQ] = {};   // of a 4-bit tile: log2(e)/sqrt(d) times the halves' sums; what undoes the power of two
     auto load_q4 = [&]() {
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
@@ -276,15 +321,16 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         e = e < 16 ? 16 : (e > 254 ? 254 : e);
         const float f = __uint_as_float((unsigned)(268 - e) << 23);        // 2^(14 - (e - 127))
         // a sum of codes * 2^-24 times queries * f, times this: the score's part in log2 units
-        qback[r] = P.scale_log2 * 16777216.f * __uint_as_float((unsigned)(e - 14) << 23);
-        qsum[r][0] = sum[0] * P.scale_log2;
-        qsum[r][1] = sum[1] * P.scale_log2;
+        const float back = P.scale_log2 * 16777216.f * __uint_as_float((unsigned)(e - 14) << 23);
+        qback[r] = of_columns(back);
+        qsum[r][0] = of_columns(sum[0] * P.scale_log2);
+        qsum[r][1] = of_columns(sum[1] * P.scale_log2);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const uint2 w = mine ? *reinterpret_cast<const uint2 *>(row + 16 * i + 4 * t) : make_uint2(0u, 0u);
           const float2 x = two<T>(w.x), y = two<T>(w.y);
-          qf[i][r] = Mma<__half>::pack(x.x * f, x.y * f);
-          qf[i][NQ + r] = Mma<__half>::pack(y.x * f * 0.0625f, y.y * f * 0.0625f);      // meets 16 times the code
+          qf[i][r][0] = Mma<__half>::pack(x.x * f, x.y * f);
+          qf[i][r][1] = Mma<__half>::pack(y.x * f * 0.0625f, y.y * f * 0.0625f);        // meets 16 times the code
         }
       }
     };
@@ -294,8 +340,8 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const T *row = qb + (g + 8 * r) * D + 16 * i + 2 * t;
-          qf[i][r] = g + 8 * r < P.G ? *reinterpret_cast<const unsigned *>(row) : 0u;
-          qf[i][NQ + r] = g + 8 * r < P.G ? *reinterpret_cast<const unsigned *>(row + 8) : 0u;
+          qf[i][r][0] = g + 8 * r < P.G ? *reinterpret_cast<const unsigned *>(row) : 0u;
+          qf[i][r][1] = g + 8 * r < P.G ? *reinterpret_cast<const unsigned *>(row + 8) : 0u;
         }
     };
     // output: rows (channels) g and g + 8 of 16, columns (queries) 2t, 2t+1 of 8.  Beside 4-bit tiles rows g are in units of
@@ -305,11 +351,10 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
-    float2 omin[NQ][2] = {};                   // sums of weight * minimum over this lane's rows (two columns), for query g (+8)
-    float m[NQ];                               // reference of the weights (log2), query g (+8)
-    float2 l[NQ] = {};                         // their sum
+    float2 omin[NQ][2] = {};                   // sums of weight * minimum over this lane's rows, for its two queries (+8)
+    float2 m[NQ], l[NQ] = {};                  // reference of the weights (log2), and their sum over this lane's rows
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) m[r] = -INFINITY;
+    for (int r = 0; r < NQ; ++r) m[r] = make_float2(-INFINITY, -INFINITY);
     float vtop = 0.f, vexp = 0.f;              // a power of two that no value scale met so far passes, and its exponent (0: none yet)
     bool in4 = false, have_q = false;
     auto to_one = [&]() {                      // output from the units of 4-bit tiles to 1
@@ -321,21 +366,34 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
           oacc[i][r][2] *= 1048576.f; oacc[i][r][3] *= 1048576.f;
         }
     };
-    // the largest of new scores of query g (+8 r) asks for a reference (all lanes together)
-    auto refer = [&](const float (&x)[NQ], float above) {
-      bool move = false;
+    auto over_rows = [&](float x) {            // the lanes that have the same columns
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) move |= x[r] + above > m[r] + kTop;
+      for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+      return x;
+    };
+    // New scores, the lane's largest of either column: the references move where any lane needs it.
+    auto refer = [&](float2 (&x)[NQ], float es) {
+      bool move = es > vtop;
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) move |= x[r].x + vexp > m[r].x + kTop || x[r].y + vexp > m[r].y + kTop;
       if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
+        for (int o = 1; o < 32; o <<= 1) es = fmaxf(es, __shfl_xor_sync(0xffffffffu, es, o));
+        if (es > vtop) {                       // a larger scale than any before
+          int e = (int)(__float_as_uint(es) >> 23) + 1;                    // es < 2^(e - 127)
+          e = e < 87 ? 87 : (e > 254 ? 254 : e);                           // not below 2^-40: sums of weights stay finite
+          vtop = __uint_as_float((unsigned)e << 23);
+          vexp = (float)(e - 127);
+        }
+#pragma unroll
         for (int r = 0; r < NQ; ++r) {
-          const float need = x[r] + above, to = need > m[r] + kTop ? need - kReset : m[r];
-          const float c = m[r] == to ? 1.f : exp2f(m[r] - to);
-          m[r] = to;
-          l[r].x *= c; l[r].y *= c;
-          omin[r][0].x *= c; omin[r][0].y *= c;
-          omin[r][1].x *= c; omin[r][1].y *= c;
-          const float c0 = __shfl_sync(0xffffffffu, c, 8 * t), c1 = __shfl_sync(0xffffffffu, c, 8 * t + 4);
+          const float n0 = over_rows(x[r].x) + vexp, n1 = over_rows(x[r].y) + vexp;
+          const float t0 = n0 > m[r].x + kTop ? n0 - kReset : m[r].x, t1 = n1 > m[r].y + kTop ? n1 - kReset : m[r].y;
+          const float c0 = m[r].x == t0 ? 1.f : exp2f(m[r].x - t0), c1 = m[r].y == t1 ? 1.f : exp2f(m[r].y - t1);
+          m[r] = make_float2(t0, t1);
+          l[r].x *= c0; l[r].y *= c1;
+          omin[r][0].x *= c0; omin[r][0].y *= c1;
+          omin[r][1].x *= c0; omin[r][1].y *= c1;
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             oacc[i][r][0] *= c0; oacc[i][r][1] *= c1;
@@ -344,108 +402,99 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         }
       }
     };
-    auto over_lanes = [&](float x) {                                       // the lanes of a query
-      x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-      return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-    };
-    // 32 rows of a 4-bit tile from `row0` of the sequence on; `first`: their place in the tile.  WHOLE: all are visible.
-    auto rows4 = [&](const unsigned char *tile_p, int first, int row0, int end, auto whole) {
+    // what is subtracted from scores (a query that has seen nothing yet only has scores of minus infinity)
+    auto minus = [&](const float2 &x) { return make_float2(x.x == -INFINITY ? 0.f : -x.x, x.y == -INFINITY ? 0.f : -x.y); };
+    // 32 rows of a 4-bit tile at shared address `tile_p`, from `row0` of the sequence on; `first`: their place in the tile.
+    // WHOLE: all are visible.
+    auto rows4 = [&](unsigned tile_p, int first, int row0, int end, auto whole) {
       constexpr bool WHOLE = decltype(whole)::value;
       auto sees = [&](int row) { return row >= 0 && row < end && (row < s.low || row >= s.high); };
-      float2 sc[NQ][4];                                                    // [16 rows, 8 rows]: the lane's two columns of 8
-      float2 vs[4][2], vm[4][2];                                           // their value scales and minima, [half]
-      float es = 0.f, top[NQ];
+      // operand row g of 8 is row `mine` of the tile's 8, so that the values' lanes (rows t and 7 - t) meet fewer bank conflicts
+      const int mine = (g & 1) ? 7 - (g >> 1) : (g >> 1);
+      const unsigned kc = tile_p + (unsigned)((first + mine) * S::kCode + t * (D / 8));
+      const unsigned kpar = tile_p + (unsigned)(2 * kRows4 * S::kCode + (first + mine) * S::kParam);
+      float2 sc[NQ][4], top[NQ];                                           // [8 rows]: the lane's row, its two queries
+      unsigned vp[4][2];                                                   // (scale, minimum) of its values, [half]
+      float es = 0.f;
 #pragma unroll
-      for (int b8 = 0; b8 < 4; ++b8) {                                     // 8 rows: columns t and 7 - t are this lane's
-        const int base = first + 8 * b8;
-        uint2 kp[2], vp[2];                                                // (scale, minimum) of either half
-        float acc[2][4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[0][e] = acc[1][e] = 0.f;
-        unsigned w[D / 32];
-        const unsigned char *codes = tile_p + (base + ((g & 1) ? 7 - (g >> 1) : (g >> 1))) * S::kCode + t * (D / 8);
-        if (D == 128) {
-          const uint4 x = *reinterpret_cast<const uint4 *>(codes);
-          w[0] = x.x; w[1] = x.y; w[D / 32 - 2] = x.z; w[D / 32 - 1] = x.w;
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2 *>(codes);
-          w[0] = x.x; w[1] = x.y;
-        }
+      for (int jj = 0; jj < 2; ++jj) {                                     // 16 rows: operand rows g and g + 8
+        unsigned w[2][D / 32];
+        uint2 kp[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const unsigned char *par = tile_p + 2 * kRows4 * S::kCode + (base + (c ? 7 - t : t)) * S::kParam;
-          kp[c] = *reinterpret_cast<const uint2 *>(par);
-          vp[c] = *reinterpret_cast<const uint2 *>(par + kRows4 * S::kParam);
+          const unsigned off = (unsigned)(16 * jj + 8 * c);
+          if (D == 128) {
+            const uint4 x = lds128(kc + off * S::kCode);
+            w[c][0] = x.x; w[c][1] = x.y; w[c][D / 32 - 2] = x.z; w[c][D / 32 - 1] = x.w;
+          } else {
+            const uint2 x = lds64(kc + off * S::kCode);
+            w[c][0] = x.x; w[c][1] = x.y;
+          }
+          kp[c] = lds64(kpar + off * S::kParam);
+          const uint2 v = lds64(kpar + (kRows4 + off) * S::kParam);
+          vp[2 * jj + c][0] = v.x; vp[2 * jj + c][1] = v.y;
         }
+        float acc[2][NQ][4];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
+        for (int i = 0; i < D / 32; ++i)
 #pragma unroll
           for (int o = 0; o < 2; ++o) {
-            const unsigned x = o ? w[i] >> 8 : w[i];
-            const int sl = 2 * i + o;
-            const unsigned a[4] = {qf[sl][0], NQ == 2 ? qf[sl][NQ - 1] : 0u, qf[sl][NQ], NQ == 2 ? qf[sl][2 * NQ - 1] : 0u};
-            Mma<__half>::run(acc[i / (D / 64)], a, x & 0x000f000fu, x & 0x00f000f0u);
-          }
-        }
-        bool vis[2] = {true, true};
-        if (!WHOLE) {
+            const unsigned x = o ? w[0][i] >> 8 : w[0][i], y = o ? w[1][i] >> 8 : w[1][i];
+            const unsigned a[4] = {x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u};
+            const int sl = 2 * i + o, u = i / (D / 64);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            vis[c] = sees(row0 + 8 * b8 + (c ? 7 - t : t));
-            if (!vis[c]) vp[c] = make_uint2(0u, 0u);
+            for (int r = 0; r < NQ; ++r) {
+              if (o == 0 && i % (D / 64) == 0) mma_first<__half>(acc[u][r], a, qf[sl][r][0], qf[sl][r][1]);
+              else Mma<__half>::run(acc[u][r], a, qf[sl][r][0], qf[sl][r][1]);
+            }
           }
-        }
-        const float2 k00 = two<T>(kp[0].x), k01 = two<T>(kp[0].y), k10 = two<T>(kp[1].x), k11 = two<T>(kp[1].y);
-        const float2 v00 = two<T>(vp[0].x), v01 = two<T>(vp[0].y), v10 = two<T>(vp[1].x), v11 = two<T>(vp[1].y);
-        vs[b8][0] = make_float2(v00.x, v10.x); vm[b8][0] = make_float2(v00.y, v10.y);
-        vs[b8][1] = make_float2(v01.x, v11.x); vm[b8][1] = make_float2(v01.y, v11.y);
-        es = fmaxf(fmaxf(es, fmaxf(v00.x, v01.x)), fmaxf(v10.x, v11.x));
 #pragma unroll
-        for (int r = 0; r < NQ; ++r) {
-          float2 part = __fmul2_rn(make_float2(k00.x, k10.x), make_float2(acc[0][2 * r], acc[0][2 * r + 1]));
-          part = __ffma2_rn(make_float2(k01.x, k11.x), make_float2(acc[1][2 * r], acc[1][2 * r + 1]), part);
-          float2 low = __fmul2_rn(make_float2(k00.y, k10.y), make_float2(qsum[r][0], qsum[r][0]));
-          low = __ffma2_rn(make_float2(k01.y, k11.y), make_float2(qsum[r][1], qsum[r][1]), low);
-          float2 x = __ffma2_rn(part, make_float2(qback[r], qback[r]), low);
+        for (int c = 0; c < 2; ++c) {
+          const int b8 = 2 * jj + c;
+          bool vis = true;
           if (!WHOLE) {
-            x.x = vis[0] ? x.x : -INFINITY;
-            x.y = vis[1] ? x.y : -INFINITY;
+            vis = sees(row0 + 8 * b8 + mine);
+            if (!vis) vp[b8][0] = vp[b8][1] = 0u;
           }
-          sc[r][b8] = x;
+          const float2 k0 = two<T>(kp[c].x), k1 = two<T>(kp[c].y);
+          es = fmaxf(es, fmaxf(two<T>(vp[b8][0]).x, two<T>(vp[b8][1]).x));
+#pragma unroll
+          for (int r = 0; r < NQ; ++r) {
+            float2 x;
+            x.x = fmaf(fmaf(k1.x, acc[1][r][2 * c], k0.x * acc[0][r][2 * c]), qback[r].x, fmaf(k1.y, qsum[r][1].x, k0.y * qsum[r][0].x));
+            x.y = fmaf(fmaf(k1.x, acc[1][r][2 * c + 1], k0.x * acc[0][r][2 * c + 1]), qback[r].y, fmaf(k1.y, qsum[r][1].y, k0.y * qsum[r][0].y));
+            if (!WHOLE && !vis) x = make_float2(-INFINITY, -INFINITY);
+            sc[r][b8] = x;
+          }
         }
       }
-#pragma unroll
-      for (int r = 0; r < NQ; ++r)
-        top[r] = over_lanes(fmaxf(fmaxf(fmaxf(sc[r][0].x, sc[r][0].y), fmaxf(sc[r][1].x, sc[r][1].y)),
-                                  fmaxf(fmaxf(sc[r][2].x, sc[r][2].y), fmaxf(sc[r][3].x, sc[r][3].y))));
-      if (__any_sync(0xffffffffu, es > vtop)) {                            // a larger scale than any before
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) es = fmaxf(es, __shfl_xor_sync(0xffffffffu, es, o));
-        int e = (int)(__float_as_uint(es) >> 23) + 1;                      // es < 2^(e - 127)
-        e = e < 87 ? 87 : (e > 254 ? 254 : e);                             // not below 2^-40: sums of weights stay finite
-        vtop = __uint_as_float((unsigned)e << 23);
-        vexp = (float)(e - 127);
-      }
-      refer(top, vexp);
-      unsigned pw[NQ][2][4];                                               // [half][8 rows]: weight * scale of two rows
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
-        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+        top[r].x = fmaxf(fmaxf(sc[r][0].x, sc[r][1].x), fmaxf(sc[r][2].x, sc[r][3].x));
+        top[r].y = fmaxf(fmaxf(sc[r][0].y, sc[r][1].y), fmaxf(sc[r][2].y, sc[r][3].y));
+      }
+      refer(top, es);
+      unsigned pw[NQ][2][4];                                               // [half][8 rows]: weight * scale as the right operand
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        const float2 ref = minus(m[r]);
 #pragma unroll
         for (int b8 = 0; b8 < 4; ++b8) {
-          const float2 x = __fadd2_rn(sc[r][b8], make_float2(-ref, -ref));
+          const float2 x = __fadd2_rn(sc[r][b8], ref);
           const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
           l[r] = __fadd2_rn(l[r], p);
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const float2 y = __fmul2_rn(p, vs[b8][u]);
-            pw[r][u][b8] = Mma<__half>::pack(y.x, y.y);
-            omin[r][u] = __ffma2_rn(p, vm[b8][u], omin[r][u]);
+            const float2 v = two<T>(vp[b8][u]);
+            pw[r][u][b8] = transposed(Mma<__half>::pack(p.x * v.x, p.y * v.x));
+            omin[r][u].x = fmaf(p.x, v.y, omin[r][u].x);
+            omin[r][u].y = fmaf(p.y, v.y, omin[r][u].y);
           }
         }
       }
-      // values: run g of the lane's rows; nibble n of a run is channel 8 n + g
-      const unsigned char *vt = tile_p + kRows4 * S::kCode + first * S::kCode + g * (D / 16);
+      // values: run g of the rows t and 7 - t of every 8; nibble n of a run is channel 8 n + g
+      const unsigned va = tile_p + (unsigned)((kRows4 + first) * S::kCode + g * (D / 16));
+      const unsigned v0 = va + (unsigned)(t * S::kCode), v1 = va + (unsigned)((7 - t) * S::kCode);
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
         unsigned w[2][2][D / 64];                                          // [8 rows][column][word]
@@ -453,12 +502,12 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const unsigned char *p = vt + (16 * jj + 8 * j + (c ? 7 - t : t)) * S::kCode;
+            const unsigned p = (c ? v1 : v0) + (unsigned)((16 * jj + 8 * j) * S::kCode);
             if (D == 128) {
-              const uint2 x = *reinterpret_cast<const uint2 *>(p);
+              const uint2 x = lds64(p);
               w[j][c][0] = x.x; w[j][c][D / 64 - 1] = x.y;
             } else {
-              w[j][c][0] = *reinterpret_cast<const unsigned *>(p);
+              w[j][c][0] = lds32(p);
             }
           }
 #pragma unroll
@@ -482,58 +531,60 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     // 16 rows of a 16-bit tile
     auto rows16 = [&](unsigned sb, int first, int row0, int end) {
       const bool whole = row0 >= 0 && row0 + 16 <= end && (row0 + 16 <= s.low || row0 >= s.high);
-      auto sees = [&](int row) { return row < end && (row < s.low || row >= s.high); };
-      float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      auto sees = [&](int row) { return whole || (row < end && (row < s.low || row >= s.high)); };
+      float acc[NQ][4];
       const int mi = lane >> 3;
       // 16-byte chunk c of row r, as the swizzled boxes of 64 channels leave it
       auto chunk_at = [&](int r, int c) { return (unsigned)((c >> 3) * S::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4)); };
 #pragma unroll
       for (int kk = 0; kk < MT; ++kk) {
-        unsigned r[4];
-        ldmatrix_x4(sb + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * kk + (mi & 1)), r);
-        const unsigned a[4] = {qf[kk][0], NQ == 2 ? qf[kk][NQ - 1] : 0u, qf[kk][NQ], NQ == 2 ? qf[kk][2 * NQ - 1] : 0u};
-        Mma<T>::run(acc[0], a, r[0], r[1]);
-        Mma<T>::run(acc[1], a, r[2], r[3]);
+        unsigned a[4];
+        ldmatrix_x4(sb + chunk_at(first + (mi & 1) * 8 + (lane & 7), 2 * kk + (mi >> 1)), a);
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) {
+          if (kk == 0) mma_first<T>(acc[r], a, qf[kk][r][0], qf[kk][r][1]);
+          else Mma<T>::run(acc[r], a, qf[kk][r][0], qf[kk][r][1]);
+        }
       }
-      float sc[NQ][4], top[NQ];
+      float2 sc[NQ][2], top[NQ];
       unsigned keep[2] = {0xffffffffu, 0xffffffffu};                       // bits of the rows 2t, 2t+1 (+ 8) that have weight
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j) {
+        if (!sees(row0 + 8 * j + 2 * t)) keep[j] &= 0xffff0000u;
+        if (!sees(row0 + 8 * j + 2 * t + 1)) keep[j] &= 0x0000ffffu;
+        const bool vis = sees(row0 + 8 * j + g);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const bool vis = whole || sees(row0 + 8 * j + 2 * t + c);
-          if (!vis) keep[j] &= c ? 0x0000ffffu : 0xffff0000u;
+        for (int r = 0; r < NQ; ++r)
+          sc[r][j] = vis ? make_float2(acc[r][2 * j] * P.scale_log2, acc[r][2 * j + 1] * P.scale_log2) : make_float2(-INFINITY, -INFINITY);
+      }
 #pragma unroll
-          for (int r = 0; r < NQ; ++r) sc[r][2 * j + c] = vis ? acc[j][2 * r + c] * P.scale_log2 : -INFINITY;
-        }
-#pragma unroll
-      for (int r = 0; r < NQ; ++r) top[r] = over_lanes(fmaxf(fmaxf(sc[r][0], sc[r][1]), fmaxf(sc[r][2], sc[r][3])));
-      refer(top, 0.f);
+      for (int r = 0; r < NQ; ++r) top[r] = make_float2(fmaxf(sc[r][0].x, sc[r][1].x) - vexp, fmaxf(sc[r][0].y, sc[r][1].y) - vexp);
+      refer(top, 0.f);                                                     // no scale beside these weights
       unsigned pw[NQ][2];
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
-        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+        const float2 ref = minus(m[r]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float p0 = exp2_fast(sc[r][2 * j] - ref), p1 = exp2_fast(sc[r][2 * j + 1] - ref);
-          l[r].x += p0;
-          l[r].y += p1;
-          pw[r][j] = Mma<T>::pack(p0, p1);
+          const float2 x = __fadd2_rn(sc[r][j], ref);
+          const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          l[r] = __fadd2_rn(l[r], p);
+          pw[r][j] = transposed(Mma<T>::pack(p.x, p.y));
         }
       }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        unsigned r[4];
-        ldmatrix_x4_trans(sb + (D / 64) * S::kBox + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * i + (mi & 1)), r);
+        unsigned v[4];
+        ldmatrix_x4_trans(sb + (D / 64) * S::kBox + chunk_at(first + (mi >> 1) * 8 + (lane & 7), 2 * i + (mi & 1)), v);
         // rows without weight may hold anything, and 0 x NaN is NaN
-        const unsigned a[4] = {r[0] & keep[0], r[1] & keep[0], r[2] & keep[1], r[3] & keep[1]};
+        const unsigned a[4] = {v[0] & keep[0], v[1] & keep[0], v[2] & keep[1], v[3] & keep[1]};
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) Mma<T>::run(oacc[i][q], a, pw[q][0], pw[q][1]);
+        for (int r = 0; r < NQ; ++r) Mma<T>::run(oacc[i][r], a, pw[r][0], pw[r][1]);
       }
     };
 
     const int lt0 = (int)(ti - at), cnt = (int)(seg_end - ti);
-    for (int i = (n ^ team) & 1; i < cnt && !failed; i += 2) {             // every second tile is this team's
+    for (int i = (team + kTeams - n % kTeams) % kTeams; i < cnt && !failed; i += kTeams) {
       const int st = (n + i) % kStages;
       if (!mbar::wait_warp(&full[st], (unsigned)((n + i) / kStages) & 1u)) {
         // a load did not arrive in time (for any lane): say so and report an empty share
@@ -548,7 +599,7 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
           const int first = 32 * (warp % kTeam), row0 = ta.row + first;
           if (row0 < end && row0 + 31 >= 0 && (row0 < s.low || row0 + 31 >= s.high)) {
             if (!in4) { load_q4(); in4 = true; }                           // kept rows come before the tail: never back
-            const unsigned char *tile_p = smem + st * S::kStage;
+            const unsigned tile_p = sbase + (unsigned)(st * S::kStage);
             if (row0 >= 0 && row0 + 32 <= end && (row0 + 32 <= s.low || row0 >= s.high)) rows4(tile_p, first, row0, end, std::true_type{});
             else rows4(tile_p, first, row0, end, std::false_type{});
           }
@@ -556,7 +607,7 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
       } else {
         // two of the team's four warps, the others on its next tile
         const int first = 16 * (warp & 1), row0 = ta.row + first;
-        if ((((warp % kTeam) >> 1) == (((n + i) >> 1) & 1)) && row0 < end && (row0 < s.low || row0 + 15 >= s.high)) {
+        if ((((warp % kTeam) >> 1) == (((n + i) / kTeams) & 1)) && row0 < end && (row0 < s.low || row0 + 15 >= s.high)) {
           if (in4 || !have_q) { load_q16(); have_q = true; }
           if (in4) { to_one(); in4 = false; }
           rows16(sbase + (unsigned)(st * S::kStage), first, row0, end);
@@ -570,7 +621,10 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     if (in4) to_one();
     if (failed) {
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) { m[r] = -INFINITY; l[r] = omin[r][0] = omin[r][1] = make_float2(0.f, 0.f); }
+      for (int r = 0; r < NQ; ++r) {
+        m[r] = make_float2(-INFINITY, -INFINITY);
+        l[r] = omin[r][0] = omin[r][1] = make_float2(0.f, 0.f);
+      }
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -581,12 +635,15 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     consumers_sync();                                                      // the merge buffer is free again
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
-      float lsum = l[r].x + l[r].y, min0 = omin[r][0].x + omin[r][0].y, min1 = omin[r][1].x + omin[r][1].y;
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        lsum += __shfl_xor_sync(0xffffffffu, lsum, o);
-        min0 += __shfl_xor_sync(0xffffffffu, min0, o);
-        min1 += __shfl_xor_sync(0xffffffffu, min1, o);
+      for (int o = 4; o < 32; o <<= 1) {
+        l[r].x += __shfl_xor_sync(0xffffffffu, l[r].x, o);
+        l[r].y += __shfl_xor_sync(0xffffffffu, l[r].y, o);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          omin[r][u].x += __shfl_xor_sync(0xffffffffu, omin[r][u].x, o);
+          omin[r][u].y += __shfl_xor_sync(0xffffffffu, omin[r][u].y, o);
+        }
       }
       float *w = mo + ((size_t)warp * kHeads + 8 * r) * S::kStride;
 #pragma unroll
@@ -596,9 +653,12 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         w[(2 * t) * S::kStride + 16 * i + 8 + g] = oacc[i][r][2];
         w[(2 * t + 1) * S::kStride + 16 * i + 8 + g] = oacc[i][r][3];
       }
-      if (t == 0) {
-        mml[warp * kHeads + 8 * r + g] = make_float2(m[r], lsum);
-        mmin[warp * kHeads + 8 * r + g] = make_float2(min0, min1);
+      if (g == 0) {
+        const int q = warp * kHeads + 8 * r + 2 * t;
+        mml[q] = make_float2(m[r].x, l[r].x);
+        mml[q + 1] = make_float2(m[r].y, l[r].y);
+        mmin[q] = make_float2(omin[r][0].x, omin[r][1].x);
+        mmin[q + 1] = make_float2(omin[r][0].y, omin[r][1].y);
       }
     }
     consumers_sync();
