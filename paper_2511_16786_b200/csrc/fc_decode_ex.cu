@@ -291,7 +291,7 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
   int n = 0;
   for (long long ti = lo; ti < hi;) {
     advance(ti);
-    const long long seg_end = at + s.tiles < hi ? at + s.tiles : hi;
+    const long long ti0 = ti, seg_end = at + s.tiles < hi ? at + s.tiles : hi;
     const T *qb = static_cast<const T *>(P.q) + ((long long)b * P.Hq + (long long)h * P.G) * D;
     // The query heads of this KV head as columns of the right operand: query g (+ 8 r), depth as the left operand's channels.
     // Scores then have rows (of the cache) as rows and queries as columns, like the output has channels and queries: what a lane
@@ -583,8 +583,13 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
       }
     };
 
-    const int lt0 = (int)(ti - at), cnt = (int)(seg_end - ti);
-    for (int i = (team + kTeams - n % kTeams) % kTeams; i < cnt && !failed; i += kTeams) {
+    const int lt0 = (int)(ti - at), cnt = (int)(seg_end - ti), team0 = n % kTeams;
+    int i = (team + kTeams - team0) % kTeams;
+    if (i < cnt) {                             // the queries, while the first tile is on its way
+      if (Q4 && lt0 + i < s.main) { load_q4(); in4 = true; }
+      else { load_q16(); have_q = true; }
+    }
+    for (; i < cnt && !failed; i += kTeams) {
       const int st = (n + i) % kStages;
       if (!mbar::wait_warp(&full[st], (unsigned)((n + i) / kStages) & 1u)) {
         // a load did not arrive in time (for any lane): say so and report an empty share
@@ -598,7 +603,6 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         if constexpr (Q4) {
           const int first = 32 * (warp % kTeam), row0 = ta.row + first;
           if (row0 < end && row0 + 31 >= 0 && (row0 < s.low || row0 + 31 >= s.high)) {
-            if (!in4) { load_q4(); in4 = true; }                           // kept rows come before the tail: never back
             const unsigned tile_p = sbase + (unsigned)(st * S::kStage);
             if (row0 >= 0 && row0 + 32 <= end && (row0 + 32 <= s.low || row0 >= s.high)) rows4(tile_p, first, row0, end, std::true_type{});
             else rows4(tile_p, first, row0, end, std::false_type{});
@@ -608,8 +612,12 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         // two of the team's four warps, the others on its next tile
         const int first = 16 * (warp & 1), row0 = ta.row + first;
         if ((((warp % kTeam) >> 1) == (((n + i) / kTeams) & 1)) && row0 < end && (row0 < s.low || row0 + 15 >= s.high)) {
-          if (in4 || !have_q) { load_q16(); have_q = true; }
-          if (in4) { to_one(); in4 = false; }
+          if (!have_q) {                                                   // kept rows come before the tail: never back
+            load_q16();
+            to_one();
+            have_q = true;
+            in4 = false;
+          }
           rows16(sbase + (unsigned)(st * S::kStage), first, row0, end);
         }
       }
@@ -631,10 +639,13 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
     }
 
-    // merge the warps
-    consumers_sync();                                                      // the merge buffer is free again
+    // merge the warps of the teams that had a tile: `parts` of them, from warp `warp0` on
+    const int parts = kTeam * (cnt < kTeams ? cnt : kTeams), warp0 = kTeam * team0;
+    const bool part = (warp + kWarps - warp0) % kWarps < parts;
+    if (ti0 > lo) consumers_sync();                                        // the merge buffer is free again
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
+      if (!part) break;
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
         l[r].x += __shfl_xor_sync(0xffffffffu, l[r].x, o);
@@ -666,22 +677,19 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     const size_t slot = ((size_t)blk + (size_t)h * P.B + b) * P.G;
     constexpr int C = D / 32;                                              // channels per lane
     for (int r = warp; r < P.G; r += kWarps) {                             // a warp per query head
-      float2 ml[kWarps];
       float mm = -INFINITY, ll = 0.f, o[C];
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) { ml[w] = mml[w * kHeads + r]; mm = fmaxf(mm, ml[w].x); }
+      for (int k = 0, w = warp0; k < parts; ++k, w = w + 1 == kWarps ? 0 : w + 1) mm = fmaxf(mm, mml[w * kHeads + r].x);
       const float ref = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
       for (int c = 0; c < C; ++c) o[c] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2f(ml[w].x - ref);
+#pragma unroll 4
+      for (int k = 0, w = warp0; k < parts; ++k, w = w + 1 == kWarps ? 0 : w + 1) {
+        const float2 ml = mml[w * kHeads + r], mn = mmin[w * kHeads + r];
+        const float f = exp2f(ml.x - ref), add = lane < 16 ? mn.x : mn.y;
         const float *src = mo + ((size_t)w * kHeads + r) * S::kStride + C * lane;
-        const float2 mn = mmin[w * kHeads + r];
-        const float add = lane < 16 ? mn.x : mn.y;
 #pragma unroll
         for (int c = 0; c < C; ++c) o[c] = fmaf(src[c] + add, f, o[c]);
-        ll = fmaf(ml[w].y, f, ll);
+        ll = fmaf(ml.y, f, ll);
       }
       if (i0 == i1) {
         const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);    // a NaN sum stays one
