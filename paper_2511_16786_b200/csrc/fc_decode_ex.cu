@@ -35,10 +35,13 @@ constexpr int kTeams = 3;                      // that take the tiles of a block
 constexpr int kWarps = kTeam * kTeams;         // consumer warps; the first of four more loads
 constexpr int kConsumers = 32 * kWarps;
 constexpr int kThreads = kConsumers + 128;
-constexpr int kRegsLoad = 32, kRegsRows = 160; // registers of a thread: 128 at launch, moved from the loading warps to the others
-static_assert(kRegsLoad + kTeams * kRegsRows <= 128 * (kTeams + 1), "a register split has to come out of what was launched");
+// Registers of a thread: 128 at launch, moved from the loading warps to the others (with 152 instead of 160 a step over 41769
+// rows of 32 heads takes 52 us instead of 49).
+constexpr int kRegsLaunch = 128, kRegsLoad = 32, kRegsRows = 160;
+static_assert(kRegsLoad + kTeams * kRegsRows <= kRegsLaunch * (kTeams + 1), "a register split has to come out of what was launched");
 constexpr int kRows4 = 32 * kTeam;             // rows of a 4-bit tile
 constexpr int kRows16 = 32;                    // rows of a 16-bit tile
+constexpr int kMaxBlocks = 256;                // blocks of a launch, at most
 constexpr float kTop = 14.f, kReset = 10.f;    // weights times the largest scale: at most 2^kTop, 2^kReset after a move
 
 struct ExParams {
@@ -68,16 +71,26 @@ struct SeqTiles {
   int a, b, main, ta, tb, tiles;               // main: tiles of kept rows in the list; ta, tb as a, b
 };
 
+// Where a sequence's rows are: in the cache [r0, r1), in the tail nt.
+struct Rows {
+  long long r0, r1;
+  int nt;
+  __device__ __forceinline__ bool operator==(const Rows &o) const { return r0 == o.r0 && r1 == o.r1 && nt == o.nt; }
+};
+__device__ __forceinline__ Rows rows_of(const ExParams &P, int i) {
+  return {__ldcg(P.offsets + i), __ldcg(P.offsets + i + 1), P.has_tail ? __ldcg(P.tail_len + i) : 0};
+}
+
 template <bool Q4>
-__device__ __forceinline__ SeqTiles seq_tiles(const ExParams &P, int i) {
+__device__ __forceinline__ SeqTiles seq_tiles(const ExParams &P, const Rows &rows) {
   constexpr int M = Q4 ? kRows4 : kRows16;
   SeqTiles s;
-  long long r0 = P.offsets[i], r1 = P.offsets[i + 1];
+  long long r0 = rows.r0, r1 = rows.r1;
+  const int nt = rows.nt;
   r1 = r1 > P.cache_rows ? P.cache_rows : r1;  // rows that the cache does not have are none
   r0 = r0 < 0 ? 0 : r0;
   s.off0 = r0;
   s.n_main = r1 > r0 ? (int)(r1 - r0) : 0;
-  const int nt = P.has_tail ? P.tail_len[i] : 0;
   s.n_tail = nt < 0 ? 0 : (nt > P.tail_cap ? P.tail_cap : nt);
   const int n = s.n_main + s.n_tail, skew = Q4 ? (int)(r0 & 1) : 0;
   s.start = r0 - skew;
@@ -120,6 +133,8 @@ __device__ __forceinline__ TileAt tile_at(const SeqTiles &s, int lt) {
   }
   return t;
 }
+
+__device__ __forceinline__ unsigned bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 
 __device__ __forceinline__ void load_bytes(void *dst, const void *src, unsigned bytes, unsigned long long *bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
@@ -202,7 +217,6 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
   const int blk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
   const int team = warp / kTeam;
 
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) { mbar::init(&full[i], 1u); mbar::init(&empty[i], kTeam); }
     mbar::init_done();
@@ -212,27 +226,39 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     if (P.has_tail) { prefetch_map(&M.tk); prefetch_map(&M.tv); }
   }
   __syncthreads();
+  // While the kernels in front still run, the share is worked out from the lengths as they are now.  It is kept if they are
+  // the same once those kernels are done, as they are but for the first step after a selection.
+  const bool few = P.B <= 32;                  // a sequence per lane
+  Rows mine = few && lane < P.B ? rows_of(P, lane) : Rows{};
+  auto share = [&]() {
+    return line::find_share(P.B, P.H, P.nb, blk, lane, [&](int i) { return seq_tiles<Q4>(P, few ? mine : rows_of(P, i)).tiles; });
+  };
+  Share sr;
+  if (few) sr = share();
   asm volatile("griddepcontrol.wait;\n" ::: "memory");       // what the kernels before this one wrote is visible from here
-
-  const Share sr = line::find_share(P.B, P.H, P.nb, blk, lane, [&](int i) { return seq_tiles<Q4>(P, i).tiles; });
+  const Rows now = few && lane < P.B ? rows_of(P, lane) : Rows{};
+  if (!few || !__all_sync(0xffffffffu, now == mine)) {
+    mine = now;
+    sr = share();
+  }
   const long long lo = sr.lo, hi = sr.hi, line_len = sr.line_len;
   const int nb = sr.nb;
   int h = sr.h, b = sr.b;
   long long at = sr.line;
   if (blk == 0)                                // sequences without rows
     for (int i = tid; i < P.B; i += kThreads)
-      if (seq_tiles<Q4>(P, i).tiles == 0) {
+      if (seq_tiles<Q4>(P, rows_of(P, i)).tiles == 0) {
         for (int hh = 0; hh < P.H; ++hh) P.span[(size_t)hh * P.B + i] = make_int2(0, -1);
         for (int c = 0; c < P.Hq * D / 8; ++c)
           reinterpret_cast<uint4 *>(static_cast<T *>(P.out) + (size_t)i * P.Hq * D)[c] = make_uint4(0u, 0u, 0u, 0u);
       }
   if (lo >= hi) return;
-  SeqTiles s = seq_tiles<Q4>(P, b);
+  SeqTiles s = seq_tiles<Q4>(P, rows_of(P, b));
   auto advance = [&](long long ti) {           // on to the sequence and head that tile ti belongs to
     while (ti >= at + s.tiles) {
       at += s.tiles;
       if (++b == P.B) { b = 0; ++h; }
-      s = seq_tiles<Q4>(P, b);
+      s = seq_tiles<Q4>(P, rows_of(P, b));
     }
   };
 
@@ -404,20 +430,20 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     };
     // what is subtracted from scores (a query that has seen nothing yet only has scores of minus infinity)
     auto minus = [&](const float2 &x) { return make_float2(x.x == -INFINITY ? 0.f : -x.x, x.y == -INFINITY ? 0.f : -x.y); };
-    // 32 rows of a 4-bit tile at shared address `tile_p`, from `row0` of the sequence on; `first`: their place in the tile.
-    // WHOLE: all are visible.
-    auto rows4 = [&](unsigned tile_p, int first, int row0, int end, auto whole) {
-      constexpr bool WHOLE = decltype(whole)::value;
-      auto sees = [&](int row) { return row >= 0 && row < end && (row < s.low || row >= s.high); };
+    // 16 JJ rows of a 4-bit tile at shared address `tile_p`, from its row `first` on.
+    // (With 16 query heads the registers are enough for 16 rows at a time.)
+    constexpr int JJ = NQ == 1 ? 2 : 1;
+    // `visible`: a bit for each of them.
+    auto rows4 = [&](unsigned tile_p, int first, unsigned visible) {
       // operand row g of 8 is row `mine` of the tile's 8, so that the values' lanes (rows t and 7 - t) meet fewer bank conflicts
       const int mine = (g & 1) ? 7 - (g >> 1) : (g >> 1);
       const unsigned kc = tile_p + (unsigned)((first + mine) * S::kCode + t * (D / 8));
       const unsigned kpar = tile_p + (unsigned)(2 * kRows4 * S::kCode + (first + mine) * S::kParam);
-      float2 sc[NQ][4], top[NQ];                                           // [8 rows]: the lane's row, its two queries
-      unsigned vp[4][2];                                                   // (scale, minimum) of its values, [half]
+      float2 sc[NQ][2 * JJ], top[NQ];                                           // [8 rows]: the lane's row, its two queries
+      unsigned vp[2 * JJ][2];                                                   // (scale, minimum) of its values, [half]
       float es = 0.f;
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {                                     // 16 rows: operand rows g and g + 8
+      for (int jj = 0; jj < JJ; ++jj) {                                     // 16 rows: operand rows g and g + 8
         unsigned w[2][D / 32];
         uint2 kp[2];
 #pragma unroll
@@ -451,35 +477,40 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int b8 = 2 * jj + c;
-          bool vis = true;
-          if (!WHOLE) {
-            vis = sees(row0 + 8 * b8 + mine);
-            if (!vis) vp[b8][0] = vp[b8][1] = 0u;
-          }
           const float2 k0 = two<T>(kp[c].x), k1 = two<T>(kp[c].y);
-          es = fmaxf(es, fmaxf(two<T>(vp[b8][0]).x, two<T>(vp[b8][1]).x));
 #pragma unroll
           for (int r = 0; r < NQ; ++r) {
             float2 x;
             x.x = fmaf(fmaf(k1.x, acc[1][r][2 * c], k0.x * acc[0][r][2 * c]), qback[r].x, fmaf(k1.y, qsum[r][1].x, k0.y * qsum[r][0].x));
             x.y = fmaf(fmaf(k1.x, acc[1][r][2 * c + 1], k0.x * acc[0][r][2 * c + 1]), qback[r].y, fmaf(k1.y, qsum[r][1].y, k0.y * qsum[r][0].y));
-            if (!WHOLE && !vis) x = make_float2(-INFINITY, -INFINITY);
             sc[r][b8] = x;
           }
         }
       }
+      if (visible != (JJ == 2 ? 0xffffffffu : 0xffffu)) {                  // seldom: an end of the rows or of the window
+#pragma unroll
+        for (int b8 = 0; b8 < 2 * JJ; ++b8)
+          if (!((visible >> (8 * b8 + mine)) & 1u)) {
+            vp[b8][0] = vp[b8][1] = 0u;
+#pragma unroll
+            for (int r = 0; r < NQ; ++r) sc[r][b8] = make_float2(-INFINITY, -INFINITY);
+          }
+      }
+#pragma unroll
+      for (int b8 = 0; b8 < 2 * JJ; ++b8) es = fmaxf(es, fmaxf(two<T>(vp[b8][0]).x, two<T>(vp[b8][1]).x));
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
-        top[r].x = fmaxf(fmaxf(sc[r][0].x, sc[r][1].x), fmaxf(sc[r][2].x, sc[r][3].x));
-        top[r].y = fmaxf(fmaxf(sc[r][0].y, sc[r][1].y), fmaxf(sc[r][2].y, sc[r][3].y));
+        top[r] = sc[r][0];
+#pragma unroll
+        for (int b8 = 1; b8 < 2 * JJ; ++b8) top[r] = make_float2(fmaxf(top[r].x, sc[r][b8].x), fmaxf(top[r].y, sc[r][b8].y));
       }
       refer(top, es);
-      unsigned pw[NQ][2][4];                                               // [half][8 rows]: weight * scale as the right operand
+      unsigned pw[NQ][2][2 * JJ];                                               // [half][8 rows]: weight * scale as the right operand
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
         const float2 ref = minus(m[r]);
 #pragma unroll
-        for (int b8 = 0; b8 < 4; ++b8) {
+        for (int b8 = 0; b8 < 2 * JJ; ++b8) {
           const float2 x = __fadd2_rn(sc[r][b8], ref);
           const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
           l[r] = __fadd2_rn(l[r], p);
@@ -496,7 +527,7 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
       const unsigned va = tile_p + (unsigned)((kRows4 + first) * S::kCode + g * (D / 16));
       const unsigned v0 = va + (unsigned)(t * S::kCode), v1 = va + (unsigned)((7 - t) * S::kCode);
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
+      for (int jj = 0; jj < JJ; ++jj) {
         unsigned w[2][2][D / 64];                                          // [8 rows][column][word]
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -601,11 +632,12 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
       const int end = ta.tail ? s.n_main + s.n_tail : s.n_main;
       if (Q4 && !ta.tail) {
         if constexpr (Q4) {
-          const int first = 32 * (warp % kTeam), row0 = ta.row + first;
-          if (row0 < end && row0 + 31 >= 0 && (row0 < s.low || row0 + 31 >= s.high)) {
-            const unsigned tile_p = sbase + (unsigned)(st * S::kStage);
-            if (row0 >= 0 && row0 + 32 <= end && (row0 + 32 <= s.low || row0 >= s.high)) rows4(tile_p, first, row0, end, std::true_type{});
-            else rows4(tile_p, first, row0, end, std::false_type{});
+#pragma unroll
+          for (int part = 0; part < 2; part += JJ) {
+            const int first = 32 * (warp % kTeam) + 16 * part, row0 = ta.row + first;
+            const unsigned there = bits_below(end - row0) & ~bits_below(-row0);
+            const unsigned visible = there & (bits_below(s.low - row0) | ~bits_below(s.high - row0)) & (JJ == 2 ? 0xffffffffu : 0xffffu);
+            if (visible) rows4(sbase + (unsigned)(st * S::kStage), first, visible);
           }
         }
       } else {
@@ -639,6 +671,9 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
     }
 
+    // Only now: blocks of the second kernel that wait on this one's SM take issue slots from it (the step over 189810 rows of 4
+    // heads 35 -> 32 us).
+    if (seg_end >= hi) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     // merge the warps of the teams that had a tile: `parts` of them, from warp `warp0` on
     const int parts = kTeam * (cnt < kTeams ? cnt : kTeams), warp0 = kTeam * team0;
     const bool part = (warp + kWarps - warp0) % kWarps < parts;
@@ -709,79 +744,68 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
 
 // out of a sequence that several blocks share: their results rescaled to the common reference and divided by the common sum.
 // Block i's result of sequence (h, b) is in slot i + h*B + b (both only ever advance along the line, so slots do not collide).
+// A block does `width` channels of a query head, all of them or, where there are few heads, a part; a thread does one, of every
+// (128 / width)th result: 16 of them are on their way at once, next to the references and sums, which every thread of the block
+// loads one or two of.
 template <typename T, int D>
 __global__ void __launch_bounds__(128)
-k_decode_ex_combine(const __grid_constant__ ExParams P) {
-  constexpr int C = D / 32, kFold = 4, kAhead = 8;
+k_decode_ex_combine(const __grid_constant__ ExParams P, int width) {
+  constexpr int kThreadsC = 128, kAhead = 16;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-  __shared__ float so[kFold][D];
-  __shared__ float2 sml[kFold];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ float weight[2 * kThreadsC], part[kThreadsC], top[4], sum[4];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = blockIdx.x / P.Hq, hq = blockIdx.x - b * P.Hq, h = hq / P.G, r = hq - h * P.G;
+  const int c = tid & (width - 1), first = tid / width, groups = kThreadsC / width;
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int2 span = __ldcg(P.span + (size_t)h * P.B + b);
   if (span.y <= span.x) return;                                            // no rows, or finished by its only block
-  const size_t slot0 = ((size_t)span.x + (size_t)h * P.B + b) * P.G + r;
   const int cnt = span.y - span.x + 1;
-  float acc[C], m = -INFINITY, l = 0.f;
+  const size_t slot0 = ((size_t)span.x + (size_t)h * P.B + b) * P.G + r;
+  const float *src = P.part_o + slot0 * D + blockIdx.y * width + c;
+  const unsigned step = (unsigned)(P.G * D);
+  float v[kAhead];
 #pragma unroll
-  for (int c = 0; c < C; ++c) acc[c] = 0.f;
-  for (int s0 = warp; s0 < cnt; s0 += kFold * kAhead) {
-    float v[kAhead][C];
-    float2 ml[kAhead];
+  for (int a = 0; a < kAhead; ++a) v[a] = first + groups * a < cnt ? __ldcg(src + (unsigned)(first + groups * a) * step) : 0.f;
+  float2 ml[2];
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const int i = s0 + a * kFold < cnt ? s0 + a * kFold : s0;
-      ml[a] = __ldcg(P.part_ml + slot0 + (size_t)i * P.G);
+  for (int e = 0; e < 2; ++e)
+    ml[e] = tid + kThreadsC * e < cnt ? __ldcg(P.part_ml + slot0 + (unsigned)(tid + kThreadsC * e) * (unsigned)P.G) : make_float2(-INFINITY, 0.f);
+  float m = fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
-      for (int c = 0; c < C; c += 2) {
-        const float2 x = __ldcg(reinterpret_cast<const float2 *>(P.part_o + (slot0 + (size_t)i * P.G) * D + C * lane + c));
-        v[a][c] = x.x; v[a][c + 1] = x.y;
-      }
-    }
-    float mn = m;
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      if (s0 + a * kFold >= cnt) ml[a] = make_float2(-INFINITY, 0.f);
-      mn = fmaxf(mn, ml[a].x);
-    }
-    const float ref = mn == -INFINITY ? 0.f : mn, keep = exp2f(m - ref);
-    m = mn;
-    l *= keep;
-#pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] *= keep;
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      if (s0 + a * kFold < cnt) {
-        const float f = exp2f(ml[a].x - ref);
-#pragma unroll
-        for (int c = 0; c < C; ++c) acc[c] = fmaf(v[a][c], f, acc[c]);
-        l = fmaf(ml[a].y, f, l);
-      }
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < C; ++c) so[warp][C * lane + c] = acc[c];
-  if (lane == 0) sml[warp] = make_float2(m, l);
+  for (int o = 1; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (lane == 0) top[warp] = m;
   __syncthreads();
-  if (warp != 0) return;
-  float mm = -INFINITY, ll = 0.f, o[C];
+  m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
 #pragma unroll
-  for (int w = 0; w < kFold; ++w) mm = fmaxf(mm, sml[w].x);
-  const float ref = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
-  for (int c = 0; c < C; ++c) o[c] = 0.f;
-#pragma unroll
-  for (int w = 0; w < kFold; ++w) {
-    const float f = exp2f(sml[w].x - ref);
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = fmaf(so[w][C * lane + c], f, o[c]);
-    ll = fmaf(sml[w].y, f, ll);
+  for (int e = 0; e < 2; ++e) {
+    const float f = exp2_fast(ml[e].x - ref);
+    weight[tid + kThreadsC * e] = f;
+    l = fmaf(f, ml[e].y, l);
   }
-  const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-  T *out = static_cast<T *>(P.out) + ((size_t)b * P.Hq + hq) * D + C * lane;
 #pragma unroll
-  for (int c = 0; c < C; c += 2) *reinterpret_cast<unsigned *>(out + c) = Mma<T>::pack(o[c] * inv, o[c + 1] * inv);
+  for (int o = 1; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  if (lane == 0) sum[warp] = l;
+  __syncthreads();
+  float acc = 0.f;
+#pragma unroll 1
+  for (int i = first;;) {
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+      if (i + groups * a < cnt) acc = fmaf(v[a], weight[i + groups * a], acc);
+    i += groups * kAhead;
+    if (i >= cnt) break;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) v[a] = i + groups * a < cnt ? __ldcg(src + (unsigned)(i + groups * a) * step) : 0.f;
+  }
+  part[tid] = acc;
+  __syncthreads();
+  if (first != 0) return;
+  for (int k = 1; k < groups; ++k) acc += part[tid + k * width];
+  l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);              // a NaN sum stays one
+  static_cast<T *>(P.out)[((size_t)b * P.Hq + hq) * D + blockIdx.y * width + c] = Mma<T>::from_float(acc * inv);
 }
 
 // ---------------------------------------------------------------------------
@@ -838,7 +862,8 @@ ExPlan plan_ex(const fc_handle *h, const fc_decode_args *a, const fc_decode_opti
   if (o->window > 0 && (long long)o->window + o->sinks < rows) rows = (long long)o->window + o->sinks;
   const long long per = (rows + size - 1) / size + 3 + (a->tail_k ? (a->tail_capacity < rows ? a->tail_capacity : rows) / kRows16 + 3 : 0);
   const long long units = (long long)a->batch * a->num_heads, tiles = units * per;
-  p.nb = (int)(tiles < h->num_sms ? tiles : h->num_sms);
+  p.nb = h->num_sms < kMaxBlocks ? h->num_sms : kMaxBlocks;
+  if (tiles < p.nb) p.nb = (int)tiles;
   const size_t slots = (size_t)(p.nb + units) * (size_t)(a->num_q_heads / a->num_heads);
   p.off_ml = (slots * a->head_dim * sizeof(float) + 255) & ~(size_t)255;
   p.off_span = p.off_ml + ((slots * sizeof(float2) + 255) & ~(size_t)255);
@@ -871,10 +896,14 @@ fc_status launch_ex(fc_handle *h, const ExParams &P, const ExMaps &M, cudaStream
   }
   fc_status s = fc_after_launch(h);
   if (s != FC_OK) return s;
-  lc.gridDim = dim3((unsigned)(P.B * P.Hq));
+  static_assert(kMaxBlocks <= 256, "the second kernel's threads take two results each");
+  // a head's channels in parts as long as there is an SM for each
+  int width = D;
+  while (width > 32 && 2ll * P.B * P.Hq * (D / width) <= h->num_sms) width /= 2;
+  lc.gridDim = dim3((unsigned)(P.B * P.Hq), (unsigned)(D / width));
   lc.blockDim = dim3(128);
   lc.dynamicSmemBytes = 0;
-  if (cudaLaunchKernelEx(&lc, k_decode_ex_combine<T, D>, P) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&lc, k_decode_ex_combine<T, D>, P, width) != cudaSuccess) {
     cudaGetLastError();
     return FC_ERR_CUDA;
   }
