@@ -499,10 +499,16 @@ def _stream_of(t: torch.Tensor) -> int:
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
-def _same_device(*tensors) -> None:
-    at = {t.device for t in tensors if t is not None}
-    if len(at) != 1 or next(iter(at)).type != "cuda":
-        raise ValueError("tensors of one CUDA device: got %s" % ", ".join(sorted(map(str, at))))
+def _same_device(first, *others) -> None:
+    at = None
+    for t in (first, *others):
+        if t is not None:
+            if at is None:
+                at = t.device
+                if at.type != "cuda":
+                    raise ValueError("tensors of one CUDA device: got %s" % at)
+            elif t.device != at:
+                raise ValueError("tensors of one CUDA device: got %s and %s" % (at, t.device))
 
 
 def _counter(t, what: str, numel: int | None = None) -> None:
@@ -527,6 +533,7 @@ class Cache4:
         self.num_heads, self.capacity_rows, self.head_dim, self.dtype = H, cap, 2 * half, params_k.dtype
         self.c = fc_cache4(codes_k.data_ptr(), codes_v.data_ptr(), params_k.data_ptr(), params_v.data_ptr(), cap,
                            _DTYPE[self.dtype], H, self.head_dim)
+        self.ref = byref(self.c)
 
     @classmethod
     def empty(cls, rows: int, num_heads: int, head_dim: int, dtype, device="cuda") -> "Cache4":
@@ -543,26 +550,31 @@ class Cache4:
 def fc_quantize_cache(handle, k, v, cache: Cache4, used=None, out_rows=None) -> None:
     """Rows k, v [rows, H, d] into 4 bits.  used: int64 [1] on the device, how many of them; out_rows: int64 [rows] on the device,
     the cache row each goes to (negative: left out)."""
-    rows = int(k.shape[0])
+    rows = k.shape[0]
     cu = (c_int32 * 2)(0, rows)
     view = make_view(k, v, cu)
     _same_device(k, v, cache.codes_k, used, out_rows)
     _counter(used, "used", 1)
     _counter(out_rows, "out_rows", rows)
-    _check(_lib.fc_quantize_cache(handle, byref(view), byref(cache.c), used.data_ptr() if used is not None else None,
-                                  out_rows.data_ptr() if out_rows is not None else None, _stream_of(k)), "fc_quantize_cache")
+    rc = _lib.fc_quantize_cache(handle, byref(view), cache.ref, None if used is None else used.data_ptr(),
+                                None if out_rows is None else out_rows.data_ptr(), _stream_of(k))
+    if rc != FC_OK:
+        raise FlashCacheError(rc, "fc_quantize_cache")
 
 
 def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
     """The values the first rows of the cache stand for into out_k, out_v [rows, H, d] (`used`: as in fc_quantize_cache)."""
-    rows = int(out_k.shape[0])
+    rows = out_k.shape[0]
+    shape = (rows, cache.num_heads, cache.head_dim)
     for o in (out_k, out_v):
-        if tuple(o.shape) != (rows, cache.num_heads, cache.head_dim) or o.dtype != cache.dtype or not o.is_contiguous():
+        if o.shape != shape or o.dtype != cache.dtype or not o.is_contiguous():
             raise ValueError("out_k/out_v: contiguous [rows, H, d] of the cache's type")
     _same_device(out_k, out_v, cache.codes_k, used)
     _counter(used, "used", 1)
-    _check(_lib.fc_dequantize_cache(handle, byref(cache.c), out_k.data_ptr(), out_v.data_ptr(), rows,
-                                    used.data_ptr() if used is not None else None, _stream_of(out_k)), "fc_dequantize_cache")
+    rc = _lib.fc_dequantize_cache(handle, cache.ref, out_k.data_ptr(), out_v.data_ptr(), rows, None if used is None else used.data_ptr(),
+                                  _stream_of(out_k))
+    if rc != FC_OK:
+        raise FlashCacheError(rc, "fc_dequantize_cache")
 
 
 def make_decode_args_ex(q, cache, offsets, max_rows: int, tail_k=None, tail_v=None, tail_len=None, window: int = 0, sinks: int = 0):

@@ -48,11 +48,16 @@ struct CacheParams {
   int H;
 };
 
-// The smallest number of the type whose 15-fold reaches hi - lo: a first guess in 32 bits, moved by what 15 times it lacks.
+// What a lane needs of its half row, and its 8 codes, code i at nibble i, where the short way below cannot be sure: exact
+// throughout, and 0 with scale 0 for a half that is all one value or not finite.
+struct Quantized { float scale; unsigned word; };
+
 template <typename T>
-__device__ __forceinline__ float scale_up(float lo, float hi) {
+__device__ __noinline__ Quantized quantize_exactly(uint4 raw, float lo, float hi) {
+  Quantized q = {0.f, 0u};
   const float d = hi - lo;
-  if (!(d > 0.f)) return 0.f;
+  if (!(d > 0.f && d < INFINITY)) return q;          // also: NaN, an infinity, a range past fp32
+  // the smallest number of the type whose 15-fold reaches hi - lo: a guess, moved by what 15 times it lacks
   const float z = d - hi;                            // two-sum: hi - lo = d + e
   const float e = (hi - (d - z)) + (-lo - z);
   auto lacks = [&](float s) { return fmaf(15.f, s, -d) - e; };       // >= 0: enough (15 s and d are multiples of ulp(d) > |e|)
@@ -60,50 +65,92 @@ __device__ __forceinline__ float scale_up(float lo, float hi) {
   if (lacks(Num<T>::to(s)) < 0.f) s = Num<T>::bits((unsigned short)(Num<T>::bits(s) + 1));
   const T below = Num<T>::bits((unsigned short)(Num<T>::bits(s) - (Num<T>::bits(s) ? 1 : 0)));
   if (lacks(Num<T>::to(below)) >= 0.f) s = below;
-  return Num<T>::to(s);
+  q.scale = Num<T>::to(s);
+  for (int i = 0; i < 8; ++i) {
+    const unsigned two = i < 4 ? (i < 2 ? raw.x : raw.y) : (i < 6 ? raw.z : raw.w);
+    const float2 both = Num<T>::both(two);
+    const float x = i & 1 ? both.y : both.x, left = x - lo;
+    unsigned k;
+    if (q.scale > 1e-30f && left + lo == x && x - left == lo) {
+      // the difference is exact, and so is the sign of what is left beside the tie above k (a quotient rounded up to a whole
+      // number is that number's, and what is left then is below the tie)
+      k = (unsigned)__float2int_rd(left / q.scale);
+      const float r = fmaf(-((float)k + 0.5f), q.scale, left);
+      if (r > 0.f || (r == 0.f && (k & 1u))) k += 1u;
+    } else {
+      const double wide = (double)x - (double)lo, h = floor(wide / (double)q.scale);
+      const double over = wide - (h + 0.5) * (double)q.scale;
+      k = (unsigned)((int)h + ((over > 0.0 || (over == 0.0 && ((int)h & 1))) ? 1 : 0));
+    }
+    q.word |= (k & 15u) << (4 * i);
+  }
+  return q;
 }
 
-// Nearest whole number of steps, ties to even.
-__device__ __forceinline__ unsigned code_of(float x, float lo, float s, float up, float inv) {
-  const float dx = (x - lo) * up, su = s * up;
-  const float m = fmaf(dx, inv, 12582912.f);         // 1.5 * 2^23: the sum's last bits are the whole number
-  float k = m - 12582912.f;
-  const float r = fmaf(-k, su, dx);
-  if (fabsf(r) >= 0.49999f * su) {                  // beside a tie, or past it: decided by the exact remainder
-    const double left = (double)x - (double)lo;
-    const double h = floor(left / (double)s);
-    const double over = left - (h + 0.5) * (double)s;
-    k = (float)h + ((over > 0.0 || (over == 0.0 && ((int)h & 1))) ? 1.f : 0.f);
+// The short way.  Scale: a fifteenth of the range in 32 bits is off by less than 2^-21 of it, so it is one of the numbers of the type
+// that both ends of that round up to.  Codes: whole numbers in the last bits of 1.5 * 2^23 + (x - lo) / scale, with a
+// quotient that is too small by up to 3e-5: they can only be one too low, at a tie or past it by that much, and what they
+// leave over (exact as long as x - lo is) tells, next to being odd at a tie itself.  Where x - lo may not be exact, because its
+// parts are 2^12 apart, and some rest is near a tie, it all goes the long way.
+template <typename T>
+__device__ __forceinline__ Quantized quantize_lane(uint4 raw, float lo, float hi) {
+  using T2 = typename Num<T>::T2;
+  const float d = hi - lo, v = d * (1.f / 15.f);
+  const float above = Num<T>::to(Num<T>::up(fmaf(v, 0x1p-21f, v))), least = Num<T>::to(Num<T>::up(fmaf(v, -0x1p-21f, v)));
+  const float z = d - hi, e = (hi - (d - z)) + (-lo - z);            // two-sum: hi - lo = d + e
+  const float s = fmaf(15.f, least, -d) - e >= 0.f ? least : above;  // is the smaller one enough (a range is often 15 steps sharp)?
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  inv = fmaf(inv, -0x1p-20f, inv);
+  const float2 lo2 = make_float2(-lo, -lo), inv2 = make_float2(inv, inv), s2 = make_float2(-s, -s), two = make_float2(2.f, 2.f);
+  const float2 big = make_float2(12582912.f, 12582912.f), gib = make_float2(-12582912.f, -12582912.f);
+  unsigned word = 0u - 0x3f400000u;                  // what the bits of 1.5 * 2^23, shifted to the nibbles, add up to
+  float most = -INFINITY;
+  const unsigned *w = reinterpret_cast<const unsigned *>(&raw);
+  const T2 *h = reinterpret_cast<const T2 *>(&raw);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = __fadd2_rn(Num<T>::both(w[i]), lo2);
+    const float2 m = __ffma2_rn(x, inv2, big);
+    const float2 past = __ffma2_rn(__ffma2_rn(__fadd2_rn(m, gib), s2, x), two, s2);          // twice the rest, less a step
+    const unsigned k0 = __float_as_uint(m.x), k1 = __float_as_uint(m.y);
+    word += k0 << (8 * i);
+    word += k1 << (8 * i + 4);
+    if (__float_as_int(past.x) + (int)(k0 & 1u) > 0) word += 1u << (8 * i);                  // > 0, or 0 at an odd one
+    if (__float_as_int(past.y) + (int)(k1 & 1u) > 0) word += 16u << (8 * i);
+    most = fmaxf(fmaxf(most, past.x), past.y);
   }
-  return (unsigned)(int)k & 15u;
+  const T2 tiny2 = __hmin2(__hmin2(__habs2(h[0]), __habs2(h[1])), __hmin2(__habs2(h[2]), __habs2(h[3])));
+  const float tiny = fminf(fminf(Num<T>::to(tiny2.x), Num<T>::to(tiny2.y)), fabsf(lo));
+  Quantized q = {s, word};
+  // v past 1e-30: neither d nor 1 / s is out of the numbers (so nothing above was NaN)
+  if (!(v > 1e-30f && v < 1e30f) || (most > -1e-4f * s && tiny < 0x1p-12f * fmaxf(fabsf(lo), fabsf(hi))))
+    q = quantize_exactly<T>(raw, lo, hi);
+  return q;
 }
 
 // One matrix's row of one head: LANES lanes with 8 channels each.
 template <typename T, int D, bool VALUES>
 __device__ __forceinline__ void quantize_row(uint4 raw, int u, unsigned char *codes, char *params, bool write) {
   constexpr int LANES = D / 8, HALF = LANES / 2;
-  const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
-  float x[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 f = Num<T>::both(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-  float lo = x[0], hi = x[0], odd = 0.f;             // odd: not 0 (NaN) once a value is not finite
-#pragma unroll
-  for (int i = 0; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); odd = fmaf(x[i], 0.f, odd); }
+  using T2 = typename Num<T>::T2;
+  const T2 *w = reinterpret_cast<const T2 *>(&raw);
+  // minimum, and minus the maximum, of the half: two 16-bit numbers in one exchange; NaN stays
+  T2 a = __hmin2_nan(__hmin2_nan(w[0], w[1]), __hmin2_nan(w[2], w[3])), b = __hmax2_nan(__hmax2_nan(w[0], w[1]), __hmax2_nan(w[2], w[3]));
+  T2 both;
+  both.x = __hmin_nan(a.x, a.y);
+  both.y = __hneg(__hmax_nan(b.x, b.y));
 #pragma unroll
   for (int o = 1; o < HALF; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    odd += __shfl_xor_sync(0xffffffffu, odd, o);
+    const unsigned other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const unsigned *>(&both), o);
+    both = __hmin2_nan(both, *reinterpret_cast<const T2 *>(&other));
   }
-  const bool finite = odd == 0.f && hi - lo < INFINITY;
-  const float s = finite ? scale_up<T>(lo, hi) : 0.f;
-  const float up = s < 1e-35f ? 1099511627776.f : 1.f;                  // 2^40: keeps the reciprocal finite
-  const float inv = s > 0.f ? 1.f / (s * up) : 0.f;
-  unsigned word = 0;                                 // code i of the lane at nibble i
-  if (s > 0.f) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) word |= code_of(x[i], lo, s, up, inv) << (4 * i);
-  }
+  const float lo = Num<T>::to(both.x), hi = -Num<T>::to(both.y);
+  const Quantized q = quantize_lane<T>(raw, lo, hi);
+  __syncwarp();
+  unsigned word = q.word;
+  const float s = q.scale;
+  const bool finite = hi - lo < INFINITY;            // not so with NaN, an infinity, or a range past fp32
   if (VALUES) {
     // nibble i of lane n -> nibble n of lane i, 8 lanes at a time: exchanges of nibbles, bytes, half-words
     unsigned o = __shfl_xor_sync(0xffffffffu, word, 1);
@@ -127,37 +174,54 @@ __device__ __forceinline__ void quantize_row(uint4 raw, int u, unsigned char *co
     if (write) *reinterpret_cast<unsigned *>(codes + t * (D / 8) + (u >> 2) * 4) = word;
   }
   if (write && (u & (HALF - 1)) == 0) {
-    const unsigned ms = Num<T>::bits(Num<T>::from(s)), ml = finite ? (unsigned)Num<T>::bits(Num<T>::from(lo)) : Num<T>::kNan;
+    const unsigned ms = Num<T>::bits(Num<T>::from(s)), ml = finite ? (unsigned)Num<T>::bits(both.x) : Num<T>::kNan;
     reinterpret_cast<unsigned *>(params)[u / HALF] = ms | (ml << 16);
   }
 }
 
+// A block does one head's rows, 256 / LANES at a time: its reads are whole rows, its writes runs of rows.
 template <typename T, int D>
-__global__ void __launch_bounds__(kQThreads)
-k_quantize(const CacheParams P) {
-  constexpr int LANES = D / 8;
+__global__ void __launch_bounds__(kQThreads, 4)
+k_quantize(const CacheParams P, int rounds) {
+  constexpr int LANES = D / 8, ROWS = kQThreads / LANES;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   long long n = P.rows;
-  if (P.used && *P.used < n) n = *P.used < 0 ? 0 : *P.used;
-  const int u = threadIdx.x % LANES;
-  const long long units = n * P.H, step = (long long)gridDim.x * (kQThreads / LANES);
-  // a warp's lanes stay together: the bound is that of its first unit
-  for (long long i0 = ((long long)blockIdx.x * kQThreads + (threadIdx.x & ~31)) / LANES; i0 < units; i0 += step) {
-    const long long i = i0 + (threadIdx.x & 31) / LANES;
-    const bool have = i < units;
-    const long long t = have ? i / P.H : 0;
-    const int h = have ? (int)(i - t * P.H) : 0;
-    const uint4 rk = __ldcs(reinterpret_cast<const uint4 *>(P.k + t * P.token + h * P.head) + u);
-    const uint4 rv = __ldcs(reinterpret_cast<const uint4 *>(P.v + t * P.token + h * P.head) + u);
-    const long long row = P.out_rows ? P.out_rows[t] : t;
-    if (have && row >= P.cap && u == 0) atomicOr(P.status, FC_DEV_FLAG_INTERNAL);
+  if (P.used) { const long long m = *P.used; n = m < n ? m : n; }
+  const unsigned h = blockIdx.x % (unsigned)P.H;
+  const int u = threadIdx.x % LANES, rows = (int)n;                   // fewer than 2^31
+  int t = (int)(blockIdx.x / (unsigned)P.H) * rounds * ROWS + threadIdx.x / LANES;
+  const int warp_row = t - (threadIdx.x & 31) / LANES;                // of the warp's first lane: a warp stays together
+  const char *k = P.k + h * P.head + t * P.token + 16 * u, *v = P.v + h * P.head + t * P.token + 16 * u;
+  const long long step = ROWS * P.token;
+  const size_t head = (size_t)h * P.cap;
+  unsigned char *ck = P.ck + head * (D / 2), *cv = P.cv + head * (D / 2);
+  char *pk = P.pk + head * cache4::kParamBytes, *pv = P.pv + head * cache4::kParamBytes;
+  uint4 rk = make_uint4(0u, 0u, 0u, 0u), rv = rk;
+  if (t < rows) { rk = __ldcs(reinterpret_cast<const uint4 *>(k)); rv = __ldcs(reinterpret_cast<const uint4 *>(v)); }
+#pragma unroll 1
+  for (int i = 0; i < rounds && warp_row + i * ROWS < rows; ++i, t += ROWS) {
+    const uint4 now_k = rk, now_v = rv;
+    if (i + 1 < rounds && t + ROWS < rows) {                          // the next rows, while these are worked on
+      k += step;
+      v += step;
+      rk = __ldcs(reinterpret_cast<const uint4 *>(k));
+      rv = __ldcs(reinterpret_cast<const uint4 *>(v));
+    }
+    const bool have = t < rows;
+    long long row = t;
+    if (P.out_rows) {
+      row = have ? P.out_rows[t] : 0;
+      if (have && row >= P.cap && u == 0) atomicOr(P.status, FC_DEV_FLAG_INTERNAL);
+    }
     const bool write = have && row >= 0 && row < P.cap;
-    const long long at = (long long)h * P.cap + (write ? row : 0);
-    quantize_row<T, D, false>(rk, u, P.ck + at * (D / 2), P.pk + at * cache4::kParamBytes, write);
-    quantize_row<T, D, true>(rv, u, P.cv + at * (D / 2), P.pv + at * cache4::kParamBytes, write);
+    const unsigned r = write ? (unsigned)row : 0u;
+    quantize_row<T, D, false>(now_k, u, ck + (size_t)r * (D / 2), pk + (size_t)r * cache4::kParamBytes, write);
+    quantize_row<T, D, true>(now_v, u, cv + (size_t)r * (D / 2), pv + (size_t)r * cache4::kParamBytes, write);
   }
 }
+
+__device__ __forceinline__ float biased(unsigned x) { return __uint_as_float(0x4b000000u | (x & 15u)); }      // 2^23 + code
 
 template <typename T, int D, bool VALUES>
 __device__ __forceinline__ uint4 values_row(const unsigned char *codes, const char *params, int u) {
@@ -185,43 +249,53 @@ __device__ __forceinline__ uint4 values_row(const unsigned char *codes, const ch
   const float2 sl = Num<T>::both(reinterpret_cast<const unsigned *>(params)[u / HALF]);
   unsigned r[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = Num<T>::pack(fmaf(sl.x, (float)((word >> (8 * i)) & 15u), sl.y), fmaf(sl.x, (float)((word >> (8 * i + 4)) & 15u), sl.y));
+  for (int i = 0; i < 4; ++i) {
+    const float2 c = __fadd2_rn(make_float2(biased(word >> (8 * i)), biased(word >> (8 * i + 4))), make_float2(-8388608.f, -8388608.f));
+    const float2 y = __ffma2_rn(c, make_float2(sl.x, sl.x), make_float2(sl.y, sl.y));
+    r[i] = Num<T>::pack(y.x, y.y);
+  }
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kQThreads)
-k_dequantize(const CacheParams P) {
-  constexpr int LANES = D / 8;
+k_dequantize(const CacheParams P, int rounds) {
+  constexpr int LANES = D / 8, ROWS = kQThreads / LANES;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   long long n = P.rows;
-  if (P.used && *P.used < n) n = *P.used < 0 ? 0 : *P.used;
-  const int u = threadIdx.x % LANES;
-  const long long units = n * P.H, step = (long long)gridDim.x * (kQThreads / LANES);
-  for (long long i0 = ((long long)blockIdx.x * kQThreads + (threadIdx.x & ~31)) / LANES; i0 < units; i0 += step) {
-    const long long i = i0 + (threadIdx.x & 31) / LANES;
-    const bool have = i < units;
-    const long long t = have ? i / P.H : 0;
-    const int h = have ? (int)(i - t * P.H) : 0;
-    const long long at = (long long)h * P.cap + t;
-    const uint4 k = values_row<T, D, false>(P.ck + at * (D / 2), P.pk + at * cache4::kParamBytes, u);
-    const uint4 v = values_row<T, D, true>(P.cv + at * (D / 2), P.pv + at * cache4::kParamBytes, u);
+  if (P.used) { const long long m = *P.used; n = m < n ? m : n; }
+  const unsigned h = blockIdx.x % (unsigned)P.H;
+  const int u = threadIdx.x % LANES, rows = (int)n;
+  int t = (int)(blockIdx.x / (unsigned)P.H) * rounds * ROWS + threadIdx.x / LANES;
+  const int warp_row = t - (threadIdx.x & 31) / LANES;
+  const size_t head = (size_t)h * P.cap;
+  const unsigned char *ck = P.ck + head * (D / 2), *cv = P.cv + head * (D / 2);
+  const char *pk = P.pk + head * cache4::kParamBytes, *pv = P.pv + head * cache4::kParamBytes;
+  uint4 *ok = reinterpret_cast<uint4 *>(P.out_k) + h * (D / 8) + u, *ov = reinterpret_cast<uint4 *>(P.out_v) + h * (D / 8) + u;
+  const size_t pitch = (size_t)P.H * (D / 8);
+#pragma unroll 2
+  for (int i = 0; i < rounds && warp_row + i * ROWS < rows; ++i, t += ROWS) {
+    const bool have = t < rows;
+    const unsigned r = have ? (unsigned)t : 0u;
+    const uint4 k = values_row<T, D, false>(ck + (size_t)r * (D / 2), pk + (size_t)r * cache4::kParamBytes, u);
+    const uint4 v = values_row<T, D, true>(cv + (size_t)r * (D / 2), pv + (size_t)r * cache4::kParamBytes, u);
     if (have) {
-      const size_t o = ((size_t)t * P.H + h) * (D / 8) + u;
-      reinterpret_cast<uint4 *>(P.out_k)[o] = k;
-      reinterpret_cast<uint4 *>(P.out_v)[o] = v;
+      ok[r * pitch] = k;
+      ov[r * pitch] = v;
     }
   }
 }
 
 template <typename K>
 fc_status launch_rows(fc_handle *h, K kern, const CacheParams &P, int D, cudaStream_t st) {
-  const long long units_per_block = kQThreads / (D / 8), blocks = (P.rows * P.H + units_per_block - 1) / units_per_block;
-  const long long most = (long long)h->num_sms * 8;                     // what fits at once: a block then walks on
+  const long long rows_per_round = kQThreads / (D / 8), rounds_all = (P.rows + rows_per_round - 1) / rows_per_round;
+  // several rounds per block, the next one's loads under way, once every SM has its blocks
+  const int rounds = rounds_all * P.H >= 4ll * 8 * h->num_sms ? 8 : (rounds_all * P.H >= 4ll * 2 * h->num_sms ? 2 : 1);
+  const long long blocks = (rounds_all + rounds - 1) / rounds * P.H;
+  if (blocks > 0x7fffffffll) return FC_ERR_UNSUPPORTED;
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
+  lc.gridDim = dim3((unsigned)blocks);
   lc.blockDim = dim3(kQThreads);
   lc.stream = st;
   cudaLaunchAttribute at[1];
@@ -229,7 +303,7 @@ fc_status launch_rows(fc_handle *h, K kern, const CacheParams &P, int D, cudaStr
   at[0].val.programmaticStreamSerializationAllowed = 1;
   lc.attrs = at;
   lc.numAttrs = 1;
-  if (cudaLaunchKernelEx(&lc, kern, P) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&lc, kern, P, rounds) != cudaSuccess) {
     cudaGetLastError();
     return FC_ERR_CUDA;
   }
