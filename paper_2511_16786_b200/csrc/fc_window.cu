@@ -35,7 +35,9 @@ constexpr int kThreadsW = 384;                 // 2 x 128: weights; then warps 8
 constexpr int kSeqs = 64;                      // sequences described per launch (kernel-argument table)
 constexpr int kValues = 4;                     // value tiles in the ring, at most
 constexpr int kSplitMin = 4;                   // key tiles that a part of a split has at least
-constexpr float kSlack = 8.f;
+// How far, in powers of two, a score may pass its row's reference before that moves (and the outputs are rescaled): weights stay
+// below 2^14 in fp16, 2^24 in bf16, and one below 2^-24 of the reference's is nothing in either.
+template <typename T> constexpr float kSlack = std::is_same<T, __half>::value ? 14.f : 24.f;
 
 struct WinSeq { int q0, nq, k0, nk, item; };   // item: first of the sequence's, in blocks before splitting
 
@@ -64,7 +66,7 @@ struct WinShape {
 
 template <int SLOTS>
 struct WinShared {
-  unsigned long long qfull, full[SLOTS], empty[SLOTS], scores[2], weights[2], done[2];
+  unsigned long long qfull, full[SLOTS], empty[SLOTS], scores[2], weights[2][2], done[2];      // weights: of the first and the last 64 keys
   // by value tile, not by slot (an odd ring holds keys and values by turns in one slot): no more than kValues of them are in it
   unsigned long long clean[kValues];
   unsigned bad[kValues][4];                    // keys of the value tile with something not finite
@@ -117,6 +119,31 @@ __device__ __forceinline__ void mma_ts(unsigned lead, unsigned d, unsigned a, un
   asm volatile("{\n .reg .pred p, q;\n .reg .b64 b;\n setp.ne.u32 q, %0, 0;\n setp.ne.u32 p, %6, 0;\n mov.b64 b, {%3, %4};\n"
                " @q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], b, %5, p;\n}\n"
                ::"r"(lead), "r"(d), "r"(a), "r"(blo), "r"(bhi), "r"(idesc), "r"(add) : "memory");
+}
+
+// Two powers of two without the special-function units, which give 16 a cycle and SM and are what the weights wait for: the
+// nearest whole number into the exponent, the rest (at most half) by the polynomial of degree 4 with the smallest largest relative
+// error on [-1/2, 1/2] (2.7e-6, found by linear programming over 4001 points).  From -126 on down it stays at 2^-126, so it is
+// for tiles without masked scores; NaN is not kept.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+  x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+  const float2 r = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));                     // 1.5 * 2^23: the last bits are the number
+  const float2 n = __fadd2_rn(r, make_float2(-12582912.f, -12582912.f));
+  const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+  float2 p = make_float2(0.009569705463945866f, 0.009569705463945866f);
+  p = __ffma2_rn(p, f, make_float2(0.05591819807887077f, 0.05591819807887077f));
+  p = __ffma2_rn(p, f, make_float2(0.24024765193462372f, 0.24024765193462372f));
+  p = __ffma2_rn(p, f, make_float2(0.6931217312812805f, 0.6931217312812805f));
+  p = __ffma2_rn(p, f, make_float2(0.9999992251396179f, 0.9999992251396179f));
+  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(r.x) << 23)),
+                     __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(r.y) << 23)));
+}
+
+// The larger one; NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -225,7 +252,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
     mbar::init(&sh.qfull, 1u);
     for (int i = 0; i < kSlots; ++i) { mbar::init(&sh.full[i], 1u); mbar::init(&sh.empty[i], 1u); }
     for (int i = 0; i < kValues; ++i) mbar::init(&sh.clean[i], 2u);
-    for (int q = 0; q < 2; ++q) { mbar::init(&sh.scores[q], 1u); mbar::init(&sh.weights[q], 4u); mbar::init(&sh.done[q], 1u); }
+    for (int q = 0; q < 2; ++q) { mbar::init(&sh.scores[q], 1u); mbar::init(&sh.weights[q][0], 4u); mbar::init(&sh.weights[q][1], 4u); mbar::init(&sh.done[q], 1u); }
     mbar::init_done();
   }
   if (warp == 8 && lane == 0) { prefetch_map(&M.q); prefetch_map(&M.k); prefetch_map(&M.v); }
@@ -299,12 +326,16 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
         for (int q = 0; q < 2 && ok; ++q) {
           if (sees_some(P, w.at[q], kt)) {
-            if (!mbar::wait_warp(&sh.weights[q], turn[q] & 1u)) { ok = false; break; }
-            ++turn[q];
-            after_sync();
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-              mma_ts(lead, tmem + 256u + 128u * q, tmem + 128u * q + 8u * c, vb + (unsigned)vs * (S::kTileBytes / 16) + 128u * c, hi, o_desc, 1u);
+            for (int half = 0; half < 2 && ok; ++half) {
+              if (!mbar::wait_warp(&sh.weights[q][half], turn[q] & 1u)) { ok = false; break; }
+              after_sync();
+#pragma unroll
+              for (int c = 4 * half; c < 4 * half + 4; ++c)
+                mma_ts(lead, tmem + 256u + 128u * q, tmem + 128u * q + 8u * c, vb + (unsigned)vs * (S::kTileBytes / 16) + 128u * c, hi, o_desc, 1u);
+            }
+            if (!ok) break;
+            ++turn[q];
           }
           if (q == 1) umma::commit(lead, &sh.empty[vs]);
           if (next) {
@@ -381,9 +412,11 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       tm_wait_st();
     }
     unsigned turn = 0u;
+    const float2 scale = make_float2(P.scale_log2, P.scale_log2);
     for (int i = 0; i < n; ++i) {
       const int kt = w.key_tile(w.u0 + i);
       if (!sees_some(P, w.at[q], kt)) continue;
+      const bool all = sees_all(P, w.at[q], kt), looked = seen_in_part(P, w, kt);
       if (!mbar::wait_warp(&sh.scores[q], turn & 1u)) { ok = false; break; }
       ++turn;
       after_sync();
@@ -391,7 +424,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
       for (int c = 0; c < 128; c += 32) tm_ld32(s_at + c, s + c);
       tm_wait_ld(s);
-      if (!sees_all(P, w.at[q], kt)) {
+      if (!all) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const unsigned bits = seen_bits(P, p, kt, c);
@@ -399,11 +432,14 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
           for (int j = 0; j < 32; ++j) s[32 * c + j] = (bits >> j) & 1u ? s[32 * c + j] : -INFINITY;
         }
       }
-      float top = s[0];
+      float tops[8];                                               // chains of their own; NaN if any score is
 #pragma unroll
-      for (int c = 1; c < 128; ++c) top = fmaxf(top, s[c]);
-      top *= P.scale_log2;
-      const bool move = top > m + kSlack;
+      for (int c = 0; c < 8; ++c) tops[c] = s[c];
+#pragma unroll
+      for (int c = 8; c < 128; ++c) tops[c & 7] = max_nan(tops[c & 7], s[c]);
+      const float top = P.scale_log2 * max_nan(max_nan(max_nan(tops[0], tops[1]), max_nan(tops[2], tops[3])),
+                                               max_nan(max_nan(tops[4], tops[5]), max_nan(tops[6], tops[7])));
+      const bool move = top > m + kSlack<T>;
       if (__any_sync(0xffffffffu, move)) {
         const float to = move ? top : m, f = m == to ? 1.f : exp2f(m - to);
         m = to;
@@ -420,24 +456,37 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
           }
         }
       }
-      const float ref = m == -INFINITY ? 0.f : m;
-      float sum = 0.f;
-#pragma unroll
-      for (int c = 0; c < 128; c += 64) {
+      const float ref = top != top ? top : (m == -INFINITY ? 0.f : m);                       // a NaN among the scores: all weights
+      const float2 minus = make_float2(-ref, -ref);
+      float2 sum = make_float2(0.f, 0.f);
+      auto weights = [&](int c, auto whole) {                      // of the keys c .. c + 63
         unsigned pk[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          const float x = exp2_fast(fmaf(s[c + 2 * j], P.scale_log2, -ref)), y = exp2_fast(fmaf(s[c + 2 * j + 1], P.scale_log2, -ref));
-          sum += x + y;
-          pk[j] = Mma<T>::pack(x, y);
+          const float2 x = __ffma2_rn(make_float2(s[c + 2 * j], s[c + 2 * j + 1]), scale, minus);
+          const float2 y = decltype(whole)::value && (j & 3) == 3 ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          sum = __fadd2_rn(sum, y);
+          pk[j] = Mma<T>::pack(y.x, y.y);
         }
         tm_st32(s_at + c / 2, pk);
-      }
-      l += sum;
-      tm_wait_st();
-      if (seen_in_part(P, w, kt)) {
+      };
+      auto ready = [&](int half) {
+        before_sync();
+        __syncwarp();
+        if (lane == 0) mbar::arrive(&sh.weights[q][half]);
+      };
+      if (!looked) {                                               // the product starts on half of them
+        weights(0, std::true_type{});
+        tm_wait_st();
+        ready(0);
+        weights(64, std::true_type{});
+        tm_wait_st();
+        ready(1);
+      } else {
+        weights(0, std::false_type{});
+        weights(64, std::false_type{});
+        tm_wait_st();
         if (!mbar::wait_warp(&sh.clean[i % kValues], (unsigned)(i / kValues) & 1u)) { ok = false; break; }
-        const bool all = sees_all(P, w.at[q], kt);
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           const unsigned mine = all ? 0xffffffffu : seen_bits(P, p, kt, c);
@@ -460,10 +509,10 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
             }
           }
         }
+        ready(0);
+        ready(1);
       }
-      before_sync();
-      __syncwarp();
-      if (lane == 0) mbar::arrive(&sh.weights[q]);
+      l += sum.x + sum.y;
     }
     if (ok) ok = mbar::wait_warp(&sh.done[q], 0u);
     if (!ok && lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
