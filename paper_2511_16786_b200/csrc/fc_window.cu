@@ -31,7 +31,6 @@ using umma::after_sync;
 using umma::before_sync;
 
 constexpr int kTileRows = 128;                 // query rows, and keys, of a tile
-constexpr int kThreadsW = 384;                 // 2 x 128: weights; then warps 8 loads, 9 products, 10 and 11 values
 constexpr int kSeqs = 64;                      // sequences described per launch (kernel-argument table)
 constexpr int kValues = 4;                     // value tiles in the ring, at most
 constexpr int kSplitMin = 4;                   // key tiles that a part of a split has at least
@@ -48,7 +47,7 @@ struct WinParams {
   int *status;
   const char *v;
   long long v_token, v_head;                   // bytes
-  int seqs, H, Hq, G, per;                     // per: queries of a tile
+  int seqs, H, Hq, G, per, tiles;              // per: queries of a tile; tiles: of a block
   int window, sinks, splits;
   float scale_log2;
   WinSeq seq[kSeqs];
@@ -56,12 +55,20 @@ struct WinParams {
 
 struct WinMaps { CUtensorMap q, k, v; };
 
+// NT query tiles to a block: two where they share what they read (128 channels); one, and two blocks to an SM, where there is room
+// for it (64): a block's beginning and end then have another's products beside them (the ragged batch of 64 channels, FIXME).
 template <int D>
 struct WinShape {
+  static constexpr int NT = D == 128 ? 2 : 1;
   static constexpr int kBox = 128 * 128;       // 128 rows of 64 channels
   static constexpr int kTileBytes = D / 64 * kBox;
-  static constexpr int kSlots = D == 128 ? 5 : 8;
-  static constexpr size_t kSmem = (size_t)(2 + kSlots) * kTileBytes + 1024;
+  static constexpr int kSlots = 5;
+  static constexpr size_t kSmem = (size_t)(NT + kSlots) * kTileBytes + 1024;
+  static constexpr int kThreads = 128 * NT + 128;                  // weights; then four warps: loads, products, values, values
+  // registers of a thread at launch, of the weights' and of the other threads
+  static constexpr int kRegs = NT == 2 ? 168 : 128, kRegsRows = NT == 2 ? 208 : 200, kRegsRest = NT == 2 ? 88 : 56;
+  static_assert(NT * kRegsRows + kRegsRest <= (NT + 1) * kRegs, "a register split has to come out of what was launched");
+  static constexpr int kColumns = NT == 2 ? 512 : 256;             // tensor memory: S of tile q at 128 q, O behind them
 };
 
 template <int SLOTS>
@@ -91,6 +98,11 @@ __device__ __forceinline__ void tm_st32(unsigned addr, const unsigned *r) {
                  "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
                  "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
                  "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tm_st16(unsigned addr, const unsigned *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
+               ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void tm_ld1(unsigned addr, unsigned &r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=r"(r) : "r"(addr));
@@ -169,15 +181,15 @@ __device__ __forceinline__ WinItem find_item(const WinParams &P, int blk) {
   int i = 0;
   while (i + 1 < P.seqs && P.seq[i + 1].item <= w.item) ++i;
   w.s = P.seq[i];
-  const int in = w.item - w.s.item, pairs = (w.s.nq + 2 * P.per - 1) / (2 * P.per);
+  const int in = w.item - w.s.item, pairs = (w.s.nq + P.tiles * P.per - 1) / (P.tiles * P.per);
   w.h = in % P.H;
-  w.first = (pairs - 1 - in / P.H) * 2 * P.per;                    // the ones that see most first
+  w.first = (pairs - 1 - in / P.H) * P.tiles * P.per;                    // the ones that see most first
   const int p0 = w.s.nk - w.s.nq;
   for (int q = 0; q < 2; ++q) {
     const int f = w.first + q * P.per, l = (f + P.per < w.s.nq ? f + P.per : w.s.nq) - 1;
     w.at[q].a = p0 + f;
     w.at[q].b = f < w.s.nq ? p0 + l : -1;
-    if (f >= w.s.nq) w.at[q].a = 0;
+    if (f >= w.s.nq || q >= P.tiles) w.at[q] = {0, -1};
   }
   const int hi = w.at[1].b > w.at[0].b ? w.at[1].b : w.at[0].b;
   int n = 0;
@@ -211,6 +223,13 @@ __device__ __forceinline__ bool seen_in_part(const WinParams &P, const WinItem &
   for (int q = 0; q < 2; ++q) part |= sees_some(P, w.at[q], kt) && !sees_all(P, w.at[q], kt);
   return part;
 }
+// 16 keys at a time: which of the tile's eight steps any row sees
+__device__ __forceinline__ unsigned seen_steps(const WinParams &P, const Span &s, int kt) {
+  const int k = kt * kTileRows, lo = (s.a < 0 ? 0 : s.a) - P.window + 1 - k, hi = s.b - k;
+  const unsigned to = hi < 0 ? 0u : (hi >= 127 ? 255u : (2u << (hi >> 4)) - 1u), from = lo <= 0 ? 0u : (lo >= 128 ? 255u : (1u << (lo >> 4)) - 1u);
+  const int sinks = P.sinks - k;
+  return to & (~from | (sinks <= 0 ? 0u : (sinks >= 128 ? 255u : (2u << ((sinks - 1) >> 4)) - 1u)));
+}
 __device__ __forceinline__ unsigned low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 // keys 32 i .. of the tile that the query at position p sees (p < 0: none)
 __device__ __forceinline__ unsigned seen_bits(const WinParams &P, int p, int kt, int i) {
@@ -237,13 +256,13 @@ template <> struct Zero2<__nv_bfloat16> {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreadsW, 1)
+__global__ void __launch_bounds__(WinShape<D>::kThreads, WinShape<D>::NT == 1 ? 2 : 1)
 k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M) {
   using S = WinShape<D>;
-  constexpr int kSlots = S::kSlots;
+  constexpr int kSlots = S::kSlots, NT = S::NT, kLoads = 4 * NT;          // kLoads: the first warp behind the weights'
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  unsigned char *ring = smem + 2 * S::kTileBytes;
+  unsigned char *ring = smem + NT * S::kTileBytes;
   __shared__ WinShared<kSlots> sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -255,23 +274,23 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
     for (int q = 0; q < 2; ++q) { mbar::init(&sh.scores[q], 1u); mbar::init(&sh.weights[q][0], 4u); mbar::init(&sh.weights[q][1], 4u); mbar::init(&sh.done[q], 1u); }
     mbar::init_done();
   }
-  if (warp == 8 && lane == 0) { prefetch_map(&M.q); prefetch_map(&M.k); prefetch_map(&M.v); }
-  if (warp == 9) umma::tmem_alloc(&sh.tmem, 512);
+  if (warp == kLoads && lane == 0) { prefetch_map(&M.q); prefetch_map(&M.k); prefetch_map(&M.v); }
+  if (warp == kLoads + 1) umma::tmem_alloc(&sh.tmem, S::kColumns);
   before_sync();
   __syncthreads();
   after_sync();
   asm volatile("griddepcontrol.wait;\n" ::: "memory");             // what the kernels before this one wrote is visible from here
-  const unsigned tmem = sh.tmem;                                   // S of tile q at 128 q, O at 256 + 128 q
+  const unsigned tmem = sh.tmem;                                   // S of tile q at 128 q, O at 128 (NT + q)
   const WinItem w = find_item(P, blockIdx.x);
   const int n = w.u1 - w.u0;
   // key tile u of the list is item 2 (u - u0) of the ring, its values the next one
   bool ok = true;
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
-    if (warp == 8) {
+  if (warp >= kLoads) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(S::kRegsRest));
+    if (warp == kLoads) {
       if (lane == 0) {
-        const int tiles_q = w.first + P.per < w.s.nq ? 2 : 1;
+        const int tiles_q = NT == 2 && w.first + P.per < w.s.nq ? 2 : 1;
         const unsigned q_bytes = (unsigned)(P.per * P.G * 128 * (D / 64));
         int items = 0;
         if (n > 0) {
@@ -292,7 +311,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         if (!ok) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
       }
       __syncwarp();
-    } else if (warp == 9) {
+    } else if (warp == kLoads + 1) {
       constexpr bool kF16 = std::is_same<T, __half>::value;
       constexpr unsigned s_desc = umma::instruction(kF16, false, kTileRows), o_desc = umma::instruction(kF16, false, D) | (1u << 16);
       constexpr unsigned hi = umma::operand_hi(1024, 2);           // 8 rows of 128 bytes each, 128-byte swizzle
@@ -313,7 +332,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         ok = mbar::wait_warp(&sh.qfull, 0u) && mbar::wait_warp(&sh.full[0], 0u);
         if (ok) {
           after_sync();
-          for (int q = 0; q < 2; ++q)
+          for (int q = 0; q < NT; ++q)
             if (sees_some(P, w.at[q], w.key_tile(w.u0))) scores(q, 0);
           umma::commit(lead, &sh.empty[0]);
         }
@@ -324,27 +343,28 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         const int kn = next ? w.key_tile(w.u0 + i + 1) : 0;
         if (!mbar::wait_warp(&sh.clean[i % kValues], (unsigned)(i / kValues) & 1u)) { ok = false; break; }
 #pragma unroll
-        for (int q = 0; q < 2 && ok; ++q) {
+        for (int q = 0; q < NT && ok; ++q) {
           if (sees_some(P, w.at[q], kt)) {
+            const unsigned steps = seen_steps(P, w.at[q], kt);
 #pragma unroll
             for (int half = 0; half < 2 && ok; ++half) {
               if (!mbar::wait_warp(&sh.weights[q][half], turn[q] & 1u)) { ok = false; break; }
               after_sync();
 #pragma unroll
               for (int c = 4 * half; c < 4 * half + 4; ++c)
-                mma_ts(lead, tmem + 256u + 128u * q, tmem + 128u * q + 8u * c, vb + (unsigned)vs * (S::kTileBytes / 16) + 128u * c, hi, o_desc, 1u);
+                if ((steps >> c) & 1u) mma_ts(lead, tmem + 128u * (NT + q), tmem + 128u * q + 8u * c, vb + (unsigned)vs * (S::kTileBytes / 16) + 128u * c, hi, o_desc, 1u);
             }
             if (!ok) break;
             ++turn[q];
           }
-          if (q == 1) umma::commit(lead, &sh.empty[vs]);
+          if (q == NT - 1) umma::commit(lead, &sh.empty[vs]);
           if (next) {
             if (q == 0) {
               if (!mbar::wait_warp(&sh.full[ki % kSlots], (unsigned)(ki / kSlots) & 1u)) { ok = false; break; }
               after_sync();
             }
             if (sees_some(P, w.at[q], kn)) scores(q, i + 1);
-            if (q == 1) umma::commit(lead, &sh.empty[ki % kSlots]);
+            if (q == NT - 1) umma::commit(lead, &sh.empty[ki % kSlots]);
           }
         }
       }
@@ -361,7 +381,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         if (seen_in_part(P, w, kt)) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int r = 64 * (warp - 10) + 32 * e + lane;
+            const int r = 64 * (warp - kLoads - 2) + 32 * e + lane;
             unsigned char *row = ring + vs * S::kTileBytes + r * 128;
             const bool past = kt * kTileRows + r >= w.s.nk;
             unsigned acc = 0u;
@@ -386,7 +406,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
               asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             }
             const unsigned which = __ballot_sync(0xffffffffu, odd);
-            if (lane == 0) sh.bad[i % kValues][2 * (warp - 10) + e] = which;
+            if (lane == 0) sh.bad[i % kValues][2 * (warp - kLoads - 2) + e] = which;
           }
         }
         __syncwarp();
@@ -395,10 +415,10 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       if (!ok && lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(S::kRegsRows));
     const int q = warp >> 2, r = (warp & 3) * 32 + lane;
     const unsigned rows = (unsigned)((warp & 3) * 32) << 16;       // this warp's lanes of tensor memory
-    const unsigned s_at = tmem + rows + 128u * q, o_at = tmem + rows + 256u + 128u * q;
+    const unsigned s_at = tmem + rows + 128u * q, o_at = tmem + rows + 128u * (NT + q);
     const int qi = w.first + q * P.per + r / P.G, head = w.h * P.G + r % P.G;
     const bool have = r < P.per * P.G && qi < w.s.nq;
     const int p = have ? w.s.nk - w.s.nq + qi : -1;
@@ -424,10 +444,13 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
       for (int c = 0; c < 128; c += 32) tm_ld32(s_at + c, s + c);
       tm_wait_ld(s);
+      unsigned chunks = 15u;                                       // 32 keys at a time: does any row of the warp see any of them
       if (!all) {
+        chunks = 0u;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const unsigned bits = seen_bits(P, p, kt, c);
+          if (__any_sync(0xffffffffu, bits != 0u)) chunks |= 1u << c;
 #pragma unroll
           for (int j = 0; j < 32; ++j) s[32 * c + j] = (bits >> j) & 1u ? s[32 * c + j] : -INFINITY;
         }
@@ -459,12 +482,12 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       const float ref = top != top ? top : (m == -INFINITY ? 0.f : m);                       // a NaN among the scores: all weights
       const float2 minus = make_float2(-ref, -ref);
       float2 sum = make_float2(0.f, 0.f);
-      auto weights = [&](int c, auto whole) {                      // of the keys c .. c + 63
+      auto weights = [&](int c) {                                  // of the keys c .. c + 63, all seen by all
         unsigned pk[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           const float2 x = __ffma2_rn(make_float2(s[c + 2 * j], s[c + 2 * j + 1]), scale, minus);
-          const float2 y = decltype(whole)::value && (j & 3) == 3 ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          const float2 y = (j & 3) == 3 ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
           sum = __fadd2_rn(sum, y);
           pk[j] = Mma<T>::pack(y.x, y.y);
         }
@@ -476,15 +499,30 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         if (lane == 0) mbar::arrive(&sh.weights[q][half]);
       };
       if (!looked) {                                               // the product starts on half of them
-        weights(0, std::true_type{});
+        weights(0);
         tm_wait_st();
         ready(0);
-        weights(64, std::true_type{});
+        weights(64);
         tm_wait_st();
         ready(1);
       } else {
-        weights(0, std::false_type{});
-        weights(64, std::false_type{});
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          unsigned pk[16];
+          if ((chunks >> c) & 1u) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float2 x = __ffma2_rn(make_float2(s[32 * c + 2 * j], s[32 * c + 2 * j + 1]), scale, minus);
+              const float2 y = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+              sum = __fadd2_rn(sum, y);
+              pk[j] = Mma<T>::pack(y.x, y.y);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) pk[j] = 0u;
+          }
+          tm_st16(s_at + 16 * c, pk);
+        }
         tm_wait_st();
         if (!mbar::wait_warp(&sh.clean[i % kValues], (unsigned)(i / kValues) & 1u)) { ok = false; break; }
 #pragma unroll 1
@@ -518,7 +556,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
     if (!ok && lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
     after_sync();
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);    // a NaN sum stays one
-    const size_t slot = (((size_t)w.item * P.splits + w.split) * 2 + q) * kTileRows + r;
+    const size_t slot = (((size_t)w.item * P.splits + w.split) * NT + q) * kTileRows + r;
 #pragma unroll 1
     for (int c = 0; c < D; c += 32) {
       float o[32];
@@ -542,7 +580,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
   before_sync();
   __syncthreads();
   after_sync();
-  if (warp == 9) umma::tmem_free(tmem, 512);
+  if (warp == kLoads + 1) umma::tmem_free(tmem, S::kColumns);
 }
 
 // Joins the parts of split blocks: a warp per row, D / 32 channels per lane.
@@ -556,7 +594,7 @@ k_window_join(const __grid_constant__ WinParams P) {
   const WinItem w = find_item(P, blockIdx.x * P.splits);
   const int qi = w.first + q * P.per + r / P.G;
   if (r >= P.per * P.G || qi >= w.s.nq) return;
-  const size_t step = 2 * kTileRows, slot0 = (size_t)w.item * P.splits * step + q * kTileRows + r;
+  const size_t step = P.tiles * kTileRows, slot0 = (size_t)w.item * P.splits * step + q * kTileRows + r;
   float m = -INFINITY;
   for (int i = 0; i < P.splits; ++i) m = fmaxf(m, __ldcg(P.part_ml + slot0 + i * step).x);
   const float ref = m == -INFINITY ? 0.f : m;
@@ -617,43 +655,46 @@ fc_status check_window(const fc_handle *h, const fc_window_args *a) {
   return FC_OK;
 }
 
+int tiles_of(int d) { return d == 128 ? WinShape<128>::NT : WinShape<64>::NT; }
+
 // One launch: sequences [b0, b1), those without queries left out.
 struct WinLaunch { int b1, items, splits, seqs; };
 
 WinLaunch plan_launch(const fc_handle *h, const fc_window_args *a, int b0, WinSeq *seq) {
   const fc_kv_view *kv = a->kv;
-  const int G = a->num_q_heads / kv->num_heads, per = kTileRows / G;
+  const int G = a->num_q_heads / kv->num_heads, per = kTileRows / G, rows = tiles_of(kv->head_dim) * per;       // queries of a block
   WinLaunch l = {b0, 0, 1, 0};
   long long items = 0, most = 0;
   for (; l.b1 < kv->batch && l.seqs < kSeqs; ++l.b1) {
     const int b = l.b1, nq = a->cu_seqlens_q[b + 1] - a->cu_seqlens_q[b], nk = kv->cu_seqlens[b + 1] - kv->cu_seqlens[b];
     if (nq == 0) continue;
-    const long long mine = (long long)((nq + 2 * per - 1) / (2 * per)) * kv->num_heads;
+    const long long mine = (long long)((nq + rows - 1) / rows) * kv->num_heads;
     if (items > 0 && items + mine > (1 << 24)) break;
     if (seq) seq[l.seqs] = {a->cu_seqlens_q[b], nq, kv->cu_seqlens[b], nk, (int)items};
     ++l.seqs;
     items += mine;
-    long long span = (long long)a->window + 2 * per + a->sinks;    // keys a block may see
+    long long span = (long long)a->window + rows + a->sinks;    // keys a block may see
     if (span > nk) span = nk;
     if (span > most) most = span;
   }
   l.items = (int)items;
   // Fewer blocks than SMs: the key tiles of each are split so that all SMs have a part, of kSplitMin tiles at least.
-  if (items > 0 && 2 * items <= h->num_sms) {
-    const long long tiles = most / kTileRows + 1, by_sm = h->num_sms / items, by_len = tiles / kSplitMin;
+  const int room = h->num_sms * (tiles_of(kv->head_dim) == 1 ? 2 : 1);
+  if (items > 0 && 2 * items <= room) {
+    const long long tiles = most / kTileRows + 1, by_sm = room / items, by_len = tiles / kSplitMin;
     l.splits = (int)(by_sm < by_len ? by_sm : by_len);
     if (l.splits < 1) l.splits = 1;
   }
   return l;
 }
 
-size_t part_bytes(const WinLaunch &l, int D) { return l.splits > 1 ? (size_t)l.items * l.splits * 2 * kTileRows * (D + 2) * sizeof(float) : 0; }
+size_t part_bytes(const WinLaunch &l, int D) { return l.splits > 1 ? (size_t)l.items * l.splits * tiles_of(D) * kTileRows * (D + 2) * sizeof(float) : 0; }
 
 template <typename T, int D>
 fc_status launch_window(fc_handle *h, const WinParams &P, const WinMaps &M, int items, cudaStream_t st) {
   using S = WinShape<D>;
   static_assert(S::kSlots <= 2 * kValues, "a value tile's turn comes again after the one before it has gone");
-  static_assert(S::kSmem + sizeof(WinShared<S::kSlots>) <= 227 * 1024, "shared memory");
+  static_assert((S::kSmem + sizeof(WinShared<S::kSlots>) + 1024) * (S::NT == 1 ? 2 : 1) <= 228 * 1024, "shared memory");
   constexpr unsigned bit = 1u << (16 + (std::is_same<T, __half>::value ? 1 : 0) + (D == 128 ? 2 : 0));
   if (!(h->forms_ready & bit)) {           // once per handle
     FC_CUDA_TRY(cudaFuncSetAttribute(k_window<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
@@ -661,7 +702,7 @@ fc_status launch_window(fc_handle *h, const WinParams &P, const WinMaps &M, int 
   }
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(items * P.splits));
-  lc.blockDim = dim3(kThreadsW);
+  lc.blockDim = dim3(S::kThreads);
   lc.dynamicSmemBytes = S::kSmem;
   lc.stream = st;
   cudaLaunchAttribute at[1];
@@ -675,7 +716,7 @@ fc_status launch_window(fc_handle *h, const WinParams &P, const WinMaps &M, int 
   }
   fc_status s = fc_after_launch(h);
   if (s != FC_OK || P.splits == 1) return s;
-  lc.gridDim = dim3((unsigned)items, (unsigned)((P.per * P.G + 3) / 4), 2);
+  lc.gridDim = dim3((unsigned)items, (unsigned)((P.per * P.G + 3) / 4), (unsigned)S::NT);
   lc.blockDim = dim3(128);
   lc.dynamicSmemBytes = 0;
   if (cudaLaunchKernelEx(&lc, k_window_join<T, D>, P) != cudaSuccess) {
@@ -723,6 +764,7 @@ extern "C" fc_status fc_window_attention(fc_handle *h, const fc_window_args *a, 
   P.Hq = a->num_q_heads;
   P.G = P.Hq / P.H;
   P.per = kTileRows / P.G;
+  P.tiles = tiles_of(D);
   P.window = a->window < (1 << 30) ? a->window : (1 << 30);
   P.sinks = a->sinks < (1 << 30) ? a->sinks : (1 << 30);
   P.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
@@ -739,7 +781,7 @@ extern "C" fc_status fc_window_attention(fc_handle *h, const fc_window_args *a, 
     P.seqs = l.seqs;
     P.splits = l.splits;
     P.part_o = static_cast<float *>(workspace);
-    P.part_ml = reinterpret_cast<float2 *>(P.part_o + (size_t)l.items * l.splits * 2 * kTileRows * D);
+    P.part_ml = reinterpret_cast<float2 *>(P.part_o + (size_t)l.items * l.splits * P.tiles * kTileRows * D);
     if (kv->dtype == FC_F16) s = D == 128 ? launch_window<__half, 128>(h, P, M, l.items, st) : launch_window<__half, 64>(h, P, M, l.items, st);
     else s = D == 128 ? launch_window<__nv_bfloat16, 128>(h, P, M, l.items, st) : launch_window<__nv_bfloat16, 64>(h, P, M, l.items, st);
     if (s != FC_OK) return s;
