@@ -151,10 +151,10 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
                      __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(r.y) << 23)));
 }
 
-// The larger one; NaN if either is.
-__device__ __forceinline__ float max_nan(float a, float b) {
+// The largest; NaN if any is.
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
@@ -264,6 +264,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char *ring = smem + NT * S::kTileBytes;
   __shared__ WinShared<kSlots> sh;
+  __shared__ WinItem item;                                         // found by one thread while others set up
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
@@ -276,12 +277,13 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
   }
   if (warp == kLoads && lane == 0) { prefetch_map(&M.q); prefetch_map(&M.k); prefetch_map(&M.v); }
   if (warp == kLoads + 1) umma::tmem_alloc(&sh.tmem, S::kColumns);
+  if (tid == 32) item = find_item(P, blockIdx.x);
   before_sync();
   __syncthreads();
   after_sync();
   asm volatile("griddepcontrol.wait;\n" ::: "memory");             // what the kernels before this one wrote is visible from here
   const unsigned tmem = sh.tmem;                                   // S of tile q at 128 q, O at 128 (NT + q)
-  const WinItem w = find_item(P, blockIdx.x);
+  const WinItem &w = item;
   const int n = w.u1 - w.u0;
   // key tile u of the list is item 2 (u - u0) of the ring, its values the next one
   bool ok = true;
@@ -444,24 +446,34 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
       for (int c = 0; c < 128; c += 32) tm_ld32(s_at + c, s + c);
       tm_wait_ld(s);
-      unsigned chunks = 15u;                                       // 32 keys at a time: does any row of the warp see any of them
-      if (!all) {
-        chunks = 0u;
+      unsigned chunks = 0u;                                        // of a tile seen in part: 32 keys at a time, those that a row of the warp sees
+      float top;                                                   // NaN if any score is
+      if (all) {
+        float tops[4] = {s[0], s[1], s[2], s[3]};                  // chains of their own
+#pragma unroll
+        for (int c = 4; c < 124; c += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tops[k] = max_nan(tops[k], s[c + 2 * k], s[c + 2 * k + 1]);
+        top = max_nan(max_nan(tops[0], s[124], s[125]), max_nan(tops[1], s[126], s[127]), max_nan(tops[2], tops[3], tops[3]));
+      } else {
+        top = -INFINITY;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const unsigned bits = seen_bits(P, p, kt, c);
-          if (__any_sync(0xffffffffu, bits != 0u)) chunks |= 1u << c;
+          if (!__any_sync(0xffffffffu, bits != 0u)) continue;
+          chunks |= 1u << c;
+          float t[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int j = 0; j < 32; ++j) s[32 * c + j] = (bits >> j) & 1u ? s[32 * c + j] : -INFINITY;
+          for (int j = 0; j < 32; j += 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[32 * c + j + k] = (bits >> (j + k)) & 1u ? s[32 * c + j + k] : -INFINITY;
+            t[0] = max_nan(t[0], s[32 * c + j], s[32 * c + j + 1]);
+            t[1] = max_nan(t[1], s[32 * c + j + 2], s[32 * c + j + 3]);
+          }
+          top = max_nan(top, t[0], t[1]);
         }
       }
-      float tops[8];                                               // chains of their own; NaN if any score is
-#pragma unroll
-      for (int c = 0; c < 8; ++c) tops[c] = s[c];
-#pragma unroll
-      for (int c = 8; c < 128; ++c) tops[c & 7] = max_nan(tops[c & 7], s[c]);
-      const float top = P.scale_log2 * max_nan(max_nan(max_nan(tops[0], tops[1]), max_nan(tops[2], tops[3])),
-                                               max_nan(max_nan(tops[4], tops[5]), max_nan(tops[6], tops[7])));
+      top *= P.scale_log2;
       const bool move = top > m + kSlack<T>;
       if (__any_sync(0xffffffffu, move)) {
         const float to = move ? top : m, f = m == to ? 1.f : exp2f(m - to);
@@ -509,7 +521,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           unsigned pk[16];
-          if ((chunks >> c) & 1u) {
+          if (all || ((chunks >> c) & 1u)) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               const float2 x = __ffma2_rn(make_float2(s[32 * c + 2 * j], s[32 * c + 2 * j + 1]), scale, minus);
@@ -694,7 +706,7 @@ template <typename T, int D>
 fc_status launch_window(fc_handle *h, const WinParams &P, const WinMaps &M, int items, cudaStream_t st) {
   using S = WinShape<D>;
   static_assert(S::kSlots <= 2 * kValues, "a value tile's turn comes again after the one before it has gone");
-  static_assert((S::kSmem + sizeof(WinShared<S::kSlots>) + 1024) * (S::NT == 1 ? 2 : 1) <= 228 * 1024, "shared memory");
+  static_assert((S::kSmem + sizeof(WinShared<S::kSlots>) + sizeof(WinItem) + 1024) * (S::NT == 1 ? 2 : 1) <= 228 * 1024, "shared memory");
   constexpr unsigned bit = 1u << (16 + (std::is_same<T, __half>::value ? 1 : 0) + (D == 128 ? 2 : 0));
   if (!(h->forms_ready & bit)) {           // once per handle
     FC_CUDA_TRY(cudaFuncSetAttribute(k_window<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
