@@ -4,8 +4,9 @@
 // no value is more than half a step off; code = (x - min) / scale to the nearest whole number, the even one of two equally
 // near.  Both are decided exactly, whatever the rounding of the arithmetic on the way: the scale by comparing 15 times a
 // candidate with the range, the code by the sign of what is left over beside a tie, in 64 bits where it is close.
-// Every row is read once and written once: bound by HBM.  A lane holds 8 consecutive channels (16 bytes), 16 or 8 lanes a
-// row of K and the same row of V; the nibbles change lanes in registers, and every lane writes one aligned word of codes.
+// Every row is read once and written once.  A lane holds 16 consecutive channels (32 bytes), 8 or 4 lanes a row of K and the same
+// row of V; the nibbles change lanes in registers, and every lane writes 8 bytes of codes.  The bytes would take FIXME; it is the
+// instructions per value that bound it.
 #include "fc_cache4.cuh"
 
 namespace {
@@ -93,50 +94,94 @@ __device__ __noinline__ Quantized quantize_exactly(uint4 raw, float lo, float hi
 // leave over (exact as long as x - lo is) tells, next to being odd at a tie itself.  Where x - lo may not be exact, because its
 // parts are 2^12 apart, and some rest is near a tie, it all goes the long way.
 template <typename T>
-__device__ __forceinline__ Quantized quantize_lane(uint4 raw, float lo, float hi) {
+__device__ __forceinline__ float quantize_lane(const uint4 (&raw)[2], float lo, float hi, unsigned (&word)[2]) {
   using T2 = typename Num<T>::T2;
   const float d = hi - lo, v = d * (1.f / 15.f);
   const float above = Num<T>::to(Num<T>::up(fmaf(v, 0x1p-21f, v))), least = Num<T>::to(Num<T>::up(fmaf(v, -0x1p-21f, v)));
   const float z = d - hi, e = (hi - (d - z)) + (-lo - z);            // two-sum: hi - lo = d + e
-  const float s = fmaf(15.f, least, -d) - e >= 0.f ? least : above;  // is the smaller one enough (a range is often 15 steps sharp)?
+  float s = fmaf(15.f, least, -d) - e >= 0.f ? least : above;        // is the smaller one enough (a range is often 15 steps sharp)?
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
   inv = fmaf(inv, -0x1p-20f, inv);
   const float2 lo2 = make_float2(-lo, -lo), inv2 = make_float2(inv, inv), s2 = make_float2(-s, -s), two = make_float2(2.f, 2.f);
   const float2 big = make_float2(12582912.f, 12582912.f), gib = make_float2(-12582912.f, -12582912.f);
-  unsigned word = 0u - 0x3f400000u;                  // what the bits of 1.5 * 2^23, shifted to the nibbles, add up to
   float most = -INFINITY;
-  const unsigned *w = reinterpret_cast<const unsigned *>(&raw);
-  const T2 *h = reinterpret_cast<const T2 *>(&raw);
+  float2 past[8];                                    // twice the rest, less a step
+  T2 tiny2;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 x = __fadd2_rn(Num<T>::both(w[i]), lo2);
-    const float2 m = __ffma2_rn(x, inv2, big);
-    const float2 past = __ffma2_rn(__ffma2_rn(__fadd2_rn(m, gib), s2, x), two, s2);          // twice the rest, less a step
-    const unsigned k0 = __float_as_uint(m.x), k1 = __float_as_uint(m.y);
-    word += k0 << (8 * i);
-    word += k1 << (8 * i + 4);
-    if (__float_as_int(past.x) + (int)(k0 & 1u) > 0) word += 1u << (8 * i);                  // > 0, or 0 at an odd one
-    if (__float_as_int(past.y) + (int)(k1 & 1u) > 0) word += 16u << (8 * i);
-    most = fmaxf(fmaxf(most, past.x), past.y);
+  for (int a = 0; a < 2; ++a) {
+    const unsigned *w = reinterpret_cast<const unsigned *>(&raw[a]);
+    const T2 *h = reinterpret_cast<const T2 *>(&raw[a]);
+    word[a] = 0u - 0x3f400000u;                      // what the bits of 1.5 * 2^23, shifted to the nibbles, add up to
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = __fadd2_rn(Num<T>::both(w[i]), lo2);
+      const float2 m = __ffma2_rn(x, inv2, big);
+      const float2 p = past[4 * a + i] = __ffma2_rn(__ffma2_rn(__fadd2_rn(m, gib), s2, x), two, s2);
+      word[a] += __float_as_uint(m.x) << (8 * i);
+      word[a] += __float_as_uint(m.y) << (8 * i + 4);
+      most = fmaxf(fmaxf(most, p.x), p.y);
+    }
+    const T2 t = __hmin2(__hmin2(__habs2(h[0]), __habs2(h[1])), __hmin2(__habs2(h[2]), __habs2(h[3])));
+    tiny2 = a ? __hmin2(tiny2, t) : t;
   }
-  const T2 tiny2 = __hmin2(__hmin2(__habs2(h[0]), __habs2(h[1])), __hmin2(__habs2(h[2]), __habs2(h[3])));
-  const float tiny = fminf(fminf(Num<T>::to(tiny2.x), Num<T>::to(tiny2.y)), fabsf(lo));
-  Quantized q = {s, word};
   // v past 1e-30: neither d nor 1 / s is out of the numbers (so nothing above was NaN)
-  if (!(v > 1e-30f && v < 1e30f) || (most > -1e-4f * s && tiny < 0x1p-12f * fmaxf(fabsf(lo), fabsf(hi))))
-    q = quantize_exactly<T>(raw, lo, hi);
-  return q;
+  const bool plain = v > 1e-30f && v < 1e30f;
+  if (!plain || most > -1e-4f * s) {
+    const float tiny = fminf(fminf(Num<T>::to(tiny2.x), Num<T>::to(tiny2.y)), fabsf(lo));
+    if (!plain || tiny < 0x1p-12f * fmaxf(fabsf(lo), fabsf(hi))) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const Quantized q = quantize_exactly<T>(raw[a], lo, hi);
+        word[a] = q.word;
+        s = q.scale;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int p = __float_as_int(i & 1 ? past[i / 2].y : past[i / 2].x);
+        const unsigned odd = (word[i / 8] >> (4 * (i % 8))) & 1u;
+        if (p + (int)odd > 0) word[i / 8] += 1u << (4 * (i % 8));    // > 0, or 0 at an odd one
+      }
+    }
+  }
+  return s;
 }
 
-// One matrix's row of one head: LANES lanes with 8 channels each.
+// Eight rows of bytes in eight lanes (four in four: MANY false), first and last four of a row in a and b: columns in the lanes'
+// place, by exchanges over one bit of the lane at a time.  Twice is nothing.
+template <bool MANY>
+__device__ __forceinline__ void turn_bytes(int u, unsigned &a, unsigned &b) {
+  if (MANY) {
+    const unsigned got = __shfl_xor_sync(0xffffffffu, u & 4 ? a : b, 4);
+    if (u & 4) a = got; else b = got;
+  }
+  unsigned got = __shfl_xor_sync(0xffffffffu, __byte_perm(a, b, u & 2 ? 0x5410 : 0x7632), 2);
+  a = __byte_perm(a, got, u & 2 ? 0x3254 : 0x5410);
+  b = __byte_perm(b, got, u & 2 ? 0x3276 : 0x7610);
+  got = __shfl_xor_sync(0xffffffffu, __byte_perm(a, b, u & 1 ? 0x6420 : 0x7531), 1);
+  a = __byte_perm(a, got, u & 1 ? 0x3514 : 0x5240);
+  b = __byte_perm(b, got, u & 1 ? 0x3716 : 0x7260);
+}
+// Nibbles of two words: the even ones of both in the first, the odd ones in the second.  Twice is nothing.
+__device__ __forceinline__ void turn_nibbles(unsigned &a, unsigned &b) {
+  const unsigned even = (a & 0x0f0f0f0fu) | ((b & 0x0f0f0f0fu) << 4), odd = ((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
+  a = even;
+  b = odd;
+}
+// Where lane u keeps its 8 bytes of a row of values: after the exchange it has run u of the even ones, then of the odd ones.
+template <int D>
+__device__ __forceinline__ int value_bytes(int u) { return D == 128 ? (u < 4 ? 2 * u : 2 * u - 7) * 8 : 8 * u; }
+
+// One matrix's row of one head: LANES lanes with 16 channels each.
 template <typename T, int D, bool VALUES>
-__device__ __forceinline__ void quantize_row(uint4 raw, int u, unsigned char *codes, char *params, bool write) {
-  constexpr int LANES = D / 8, HALF = LANES / 2;
+__device__ __forceinline__ void quantize_row(const uint4 (&raw)[2], int u, unsigned char *codes, char *params, bool write) {
+  constexpr int LANES = D / 16, HALF = LANES / 2;
   using T2 = typename Num<T>::T2;
-  const T2 *w = reinterpret_cast<const T2 *>(&raw);
+  const T2 *w = reinterpret_cast<const T2 *>(&raw[0]);
   // minimum, and minus the maximum, of the half: two 16-bit numbers in one exchange; NaN stays
-  T2 a = __hmin2_nan(__hmin2_nan(w[0], w[1]), __hmin2_nan(w[2], w[3])), b = __hmax2_nan(__hmax2_nan(w[0], w[1]), __hmax2_nan(w[2], w[3]));
+  T2 a = __hmin2_nan(__hmin2_nan(__hmin2_nan(w[0], w[1]), __hmin2_nan(w[2], w[3])), __hmin2_nan(__hmin2_nan(w[4], w[5]), __hmin2_nan(w[6], w[7])));
+  T2 b = __hmax2_nan(__hmax2_nan(__hmax2_nan(w[0], w[1]), __hmax2_nan(w[2], w[3])), __hmax2_nan(__hmax2_nan(w[4], w[5]), __hmax2_nan(w[6], w[7])));
   T2 both;
   both.x = __hmin_nan(a.x, a.y);
   both.y = __hneg(__hmax_nan(b.x, b.y));
@@ -146,32 +191,28 @@ __device__ __forceinline__ void quantize_row(uint4 raw, int u, unsigned char *co
     both = __hmin2_nan(both, *reinterpret_cast<const T2 *>(&other));
   }
   const float lo = Num<T>::to(both.x), hi = -Num<T>::to(both.y);
-  const Quantized q = quantize_lane<T>(raw, lo, hi);
+  unsigned word[2];
+  const float s = quantize_lane<T>(raw, lo, hi, word);
   __syncwarp();
-  unsigned word = q.word;
-  const float s = q.scale;
   const bool finite = hi - lo < INFINITY;            // not so with NaN, an infinity, or a range past fp32
   if (VALUES) {
-    // nibble i of lane n -> nibble n of lane i, 8 lanes at a time: exchanges of nibbles, bytes, half-words
-    unsigned o = __shfl_xor_sync(0xffffffffu, word, 1);
-    word = (u & 1) ? ((word & 0xf0f0f0f0u) | ((o >> 4) & 0x0f0f0f0fu)) : ((word & 0x0f0f0f0fu) | ((o << 4) & 0xf0f0f0f0u));
-    o = __shfl_xor_sync(0xffffffffu, word, 2);
-    word = (u & 2) ? ((word & 0xff00ff00u) | ((o >> 8) & 0x00ff00ffu)) : ((word & 0x00ff00ffu) | ((o << 8) & 0xff00ff00u));
-    o = __shfl_xor_sync(0xffffffffu, word, 4);
-    word = (u & 4) ? ((word & 0xffff0000u) | (o >> 16)) : ((word & 0x0000ffffu) | (o << 16));
-    if (write) *reinterpret_cast<unsigned *>(codes + (u & 7) * (D / 16) + (u >> 3) * 4) = word;
+    turn_nibbles(word[0], word[1]);
+    turn_bytes<D == 128>(u, word[0], word[1]);
+    if (write) *reinterpret_cast<uint2 *>(codes + value_bytes<D>(u)) = make_uint2(word[0], word[1]);
   } else {
-    // two quads of one slice, of runs t and t + 1, t = 2 (u & 1); the lane that has the other slice of the words is u ^ 2
-    const int odd_slice = (u >> 1) & 1;
-    auto spread = [&](unsigned q) {                  // i = 0..3 -> nibbles 0, 4, 1, 5 (odd slices: 2 more)
-      const unsigned v = (q & 0xfu) | ((q & 0xf0u) << 12) | ((q & 0xf00u) >> 4) | ((q & 0xf000u) << 8);
-      return v << (8 * odd_slice);
+    // the lane's slice has a quad for each run; the neighbour has the other slice of the words.  An even lane makes the words of
+    // runs 0 and 1, an odd one of 2 and 3.
+    const bool odd = u & 1;
+    const unsigned got = __shfl_xor_sync(0xffffffffu, odd ? word[0] : word[1], 1), mine = odd ? word[1] : word[0];
+    const unsigned first = odd ? got : mine, second = odd ? mine : got;                      // of the even slice, of the odd one
+    auto spread = [](unsigned q) {                   // i = 0..3 -> nibbles 0, 4, 1, 5
+      return (q & 0xfu) | ((q & 0xf0u) << 12) | ((q & 0xf00u) >> 4) | ((q & 0xf000u) << 8);
     };
-    const unsigned q0 = spread(word & 0xffffu), q1 = spread(word >> 16);
-    const unsigned got = __shfl_xor_sync(0xffffffffu, odd_slice ? q0 : q1, 2);
-    word = (odd_slice ? q1 : q0) | got;
-    const int t = 2 * (u & 1) + odd_slice;
-    if (write) *reinterpret_cast<unsigned *>(codes + t * (D / 8) + (u >> 2) * 4) = word;
+    if (write) {
+      unsigned char *at = codes + 2 * odd * (D / 8) + (u >> 1) * 4;
+      *reinterpret_cast<unsigned *>(at) = spread(first) | (spread(second) << 8);
+      *reinterpret_cast<unsigned *>(at + D / 8) = spread(first >> 16) | (spread(second >> 16) << 8);
+    }
   }
   if (write && (u & (HALF - 1)) == 0) {
     const unsigned ms = Num<T>::bits(Num<T>::from(s)), ml = finite ? (unsigned)Num<T>::bits(both.x) : Num<T>::kNan;
@@ -183,7 +224,7 @@ __device__ __forceinline__ void quantize_row(uint4 raw, int u, unsigned char *co
 template <typename T, int D>
 __global__ void __launch_bounds__(kQThreads, 4)
 k_quantize(const CacheParams P, int rounds) {
-  constexpr int LANES = D / 8, ROWS = kQThreads / LANES;
+  constexpr int LANES = D / 16, ROWS = kQThreads / LANES;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   long long n = P.rows;
@@ -192,21 +233,27 @@ k_quantize(const CacheParams P, int rounds) {
   const int u = threadIdx.x % LANES, rows = (int)n;                   // fewer than 2^31
   int t = (int)(blockIdx.x / (unsigned)P.H) * rounds * ROWS + threadIdx.x / LANES;
   const int warp_row = t - (threadIdx.x & 31) / LANES;                // of the warp's first lane: a warp stays together
-  const char *k = P.k + h * P.head + t * P.token + 16 * u, *v = P.v + h * P.head + t * P.token + 16 * u;
+  const char *k = P.k + h * P.head + t * P.token + 32 * u, *v = P.v + h * P.head + t * P.token + 32 * u;
   const long long step = ROWS * P.token;
   const size_t head = (size_t)h * P.cap;
   unsigned char *ck = P.ck + head * (D / 2), *cv = P.cv + head * (D / 2);
   char *pk = P.pk + head * cache4::kParamBytes, *pv = P.pv + head * cache4::kParamBytes;
-  uint4 rk = make_uint4(0u, 0u, 0u, 0u), rv = rk;
-  if (t < rows) { rk = __ldcs(reinterpret_cast<const uint4 *>(k)); rv = __ldcs(reinterpret_cast<const uint4 *>(v)); }
+  uint4 rk[2] = {}, rv[2] = {};
+  auto fetch = [&]() {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      rk[a] = __ldcs(reinterpret_cast<const uint4 *>(k) + a);
+      rv[a] = __ldcs(reinterpret_cast<const uint4 *>(v) + a);
+    }
+  };
+  if (t < rows) fetch();
 #pragma unroll 1
   for (int i = 0; i < rounds && warp_row + i * ROWS < rows; ++i, t += ROWS) {
-    const uint4 now_k = rk, now_v = rv;
+    const uint4 now_k[2] = {rk[0], rk[1]}, now_v[2] = {rv[0], rv[1]};
     if (i + 1 < rounds && t + ROWS < rows) {                          // the next rows, while these are worked on
       k += step;
       v += step;
-      rk = __ldcs(reinterpret_cast<const uint4 *>(k));
-      rv = __ldcs(reinterpret_cast<const uint4 *>(v));
+      fetch();
     }
     const bool have = t < rows;
     long long row = t;
@@ -224,43 +271,45 @@ k_quantize(const CacheParams P, int rounds) {
 __device__ __forceinline__ float biased(unsigned x) { return __uint_as_float(0x4b000000u | (x & 15u)); }      // 2^23 + code
 
 template <typename T, int D, bool VALUES>
-__device__ __forceinline__ uint4 values_row(const unsigned char *codes, const char *params, int u) {
-  constexpr int HALF = D / 16;
-  unsigned word;                                     // code i of the lane at nibble i: the steps above backwards
+__device__ __forceinline__ void values_row(const unsigned char *codes, const char *params, int u, uint4 (&out)[2]) {
+  constexpr int HALF = D / 32;
+  unsigned word[2];                                  // code i of the lane at nibble i: the steps above backwards
   if (VALUES) {
-    word = *reinterpret_cast<const unsigned *>(codes + (u & 7) * (D / 16) + (u >> 3) * 4);
-    unsigned o = __shfl_xor_sync(0xffffffffu, word, 4);
-    word = (u & 4) ? ((word & 0xffff0000u) | (o >> 16)) : ((word & 0x0000ffffu) | (o << 16));
-    o = __shfl_xor_sync(0xffffffffu, word, 2);
-    word = (u & 2) ? ((word & 0xff00ff00u) | ((o >> 8) & 0x00ff00ffu)) : ((word & 0x00ff00ffu) | ((o << 8) & 0xff00ff00u));
-    o = __shfl_xor_sync(0xffffffffu, word, 1);
-    word = (u & 1) ? ((word & 0xf0f0f0f0u) | ((o >> 4) & 0x0f0f0f0fu)) : ((word & 0x0f0f0f0fu) | ((o << 4) & 0xf0f0f0f0u));
+    const uint2 x = *reinterpret_cast<const uint2 *>(codes + value_bytes<D>(u));
+    word[0] = x.x;
+    word[1] = x.y;
+    turn_bytes<D == 128>(u, word[0], word[1]);
+    turn_nibbles(word[0], word[1]);
   } else {
-    const int odd_slice = (u >> 1) & 1, t = 2 * (u & 1) + odd_slice;
-    word = *reinterpret_cast<const unsigned *>(codes + t * (D / 8) + (u >> 2) * 4);
-    const unsigned mine = (word >> (8 * odd_slice)) & 0x00ff00ffu, theirs = (word >> (8 - 8 * odd_slice)) & 0x00ff00ffu;
-    const unsigned got = __shfl_xor_sync(0xffffffffu, theirs, 2);
+    const bool odd = u & 1;
+    const unsigned char *at = codes + 2 * odd * (D / 8) + (u >> 1) * 4;
+    const unsigned a = *reinterpret_cast<const unsigned *>(at), b = *reinterpret_cast<const unsigned *>(at + D / 8);
     auto gather = [](unsigned v) {                   // nibbles 0, 4, 1, 5 -> 0, 1, 2, 3
       return (v & 0xfu) | ((v >> 12) & 0xf0u) | ((v << 4) & 0xf00u) | ((v >> 8) & 0xf000u);
     };
-    const unsigned a = gather(mine), b = gather(got);
-    word = odd_slice ? (b | (a << 16)) : (a | (b << 16));
+    const unsigned first = gather(a) | (gather(b) << 16), second = gather(a >> 8) | (gather(b >> 8) << 16);
+    const unsigned got = __shfl_xor_sync(0xffffffffu, odd ? first : second, 1);
+    word[0] = odd ? got : first;
+    word[1] = odd ? second : got;
   }
   const float2 sl = Num<T>::both(reinterpret_cast<const unsigned *>(params)[u / HALF]);
-  unsigned r[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 c = __fadd2_rn(make_float2(biased(word >> (8 * i)), biased(word >> (8 * i + 4))), make_float2(-8388608.f, -8388608.f));
-    const float2 y = __ffma2_rn(c, make_float2(sl.x, sl.x), make_float2(sl.y, sl.y));
-    r[i] = Num<T>::pack(y.x, y.y);
+  for (int a = 0; a < 2; ++a) {
+    unsigned r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 c = __fadd2_rn(make_float2(biased(word[a] >> (8 * i)), biased(word[a] >> (8 * i + 4))), make_float2(-8388608.f, -8388608.f));
+      const float2 y = __ffma2_rn(c, make_float2(sl.x, sl.x), make_float2(sl.y, sl.y));
+      r[i] = Num<T>::pack(y.x, y.y);
+    }
+    out[a] = make_uint4(r[0], r[1], r[2], r[3]);
   }
-  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kQThreads)
 k_dequantize(const CacheParams P, int rounds) {
-  constexpr int LANES = D / 8, ROWS = kQThreads / LANES;
+  constexpr int LANES = D / 16, ROWS = kQThreads / LANES;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   long long n = P.rows;
@@ -272,24 +321,28 @@ k_dequantize(const CacheParams P, int rounds) {
   const size_t head = (size_t)h * P.cap;
   const unsigned char *ck = P.ck + head * (D / 2), *cv = P.cv + head * (D / 2);
   const char *pk = P.pk + head * cache4::kParamBytes, *pv = P.pv + head * cache4::kParamBytes;
-  uint4 *ok = reinterpret_cast<uint4 *>(P.out_k) + h * (D / 8) + u, *ov = reinterpret_cast<uint4 *>(P.out_v) + h * (D / 8) + u;
+  uint4 *ok = reinterpret_cast<uint4 *>(P.out_k) + h * (D / 8) + 2 * u, *ov = reinterpret_cast<uint4 *>(P.out_v) + h * (D / 8) + 2 * u;
   const size_t pitch = (size_t)P.H * (D / 8);
 #pragma unroll 2
   for (int i = 0; i < rounds && warp_row + i * ROWS < rows; ++i, t += ROWS) {
     const bool have = t < rows;
     const unsigned r = have ? (unsigned)t : 0u;
-    const uint4 k = values_row<T, D, false>(ck + (size_t)r * (D / 2), pk + (size_t)r * cache4::kParamBytes, u);
-    const uint4 v = values_row<T, D, true>(cv + (size_t)r * (D / 2), pv + (size_t)r * cache4::kParamBytes, u);
+    uint4 k[2], v[2];
+    values_row<T, D, false>(ck + (size_t)r * (D / 2), pk + (size_t)r * cache4::kParamBytes, u, k);
+    values_row<T, D, true>(cv + (size_t)r * (D / 2), pv + (size_t)r * cache4::kParamBytes, u, v);
     if (have) {
-      ok[r * pitch] = k;
-      ov[r * pitch] = v;
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        ok[r * pitch + a] = k[a];
+        ov[r * pitch + a] = v[a];
+      }
     }
   }
 }
 
 template <typename K>
 fc_status launch_rows(fc_handle *h, K kern, const CacheParams &P, int D, cudaStream_t st) {
-  const long long rows_per_round = kQThreads / (D / 8), rounds_all = (P.rows + rows_per_round - 1) / rows_per_round;
+  const long long rows_per_round = kQThreads / (D / 16), rounds_all = (P.rows + rows_per_round - 1) / rows_per_round;
   // several rounds per block, the next one's loads under way, once every SM has its blocks
   const int rounds = rounds_all * P.H >= 4ll * 8 * h->num_sms ? 8 : (rounds_all * P.H >= 4ll * 2 * h->num_sms ? 2 : 1);
   const long long blocks = (rounds_all + rounds - 1) / rounds * P.H;

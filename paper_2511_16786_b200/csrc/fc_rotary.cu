@@ -126,8 +126,9 @@ template <typename T>
 fc_status launch_rotary(fc_handle *h, const RotParams &P, bool inter, cudaStream_t st) {
   constexpr int W = 16 / (int)sizeof(T);
   const bool wide = P.R % (2 * W) == 0;
-  // Several tokens per block once every SM has a few blocks anyway: fewer blocks, more loads in flight in each.
-  const int tb = P.T > 4ll * h->num_sms ? 4 : 1;
+  // Two tokens to a block where the blocks come in many waves (32768 tokens of 32 heads 102 -> 94 us, 4 and 8 tokens 94 and 100),
+  // else one (5001 tokens of 64 heads 28 us; 29, 33 and 47 with 2, 4 and 8: fewer blocks fill the last wave worse).
+  const int tb = P.T > 64ll * h->num_sms ? 2 : 1;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((P.T + tb - 1) / tb));
   lc.blockDim = dim3(kRotThreads);
