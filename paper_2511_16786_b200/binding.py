@@ -550,12 +550,15 @@ class Cache4:
 def fc_quantize_cache(handle, k, v, cache: Cache4, used=None, out_rows=None) -> None:
     """Rows k, v [rows, H, d] into 4 bits.  used: int64 [1] on the device, how many of them; out_rows: int64 [rows] on the device,
     the cache row each goes to (negative: left out)."""
-    rows = k.shape[0]
-    cu = (c_int32 * 2)(0, rows)
-    view = make_view(k, v, cu)
+    rows, strides, dtype = k.shape[0], k.stride(), k.dtype
+    if k.dim() != 3 or v.shape != k.shape or v.dtype != dtype or v.stride() != strides or strides[2] != 1 or dtype not in _DTYPE:
+        raise ValueError("k and v: [rows, H, d] of one dtype, laid out alike, channel stride 1")
     _same_device(k, v, cache.codes_k, used, out_rows)
     _counter(used, "used", 1)
     _counter(out_rows, "out_rows", rows)
+    cu = (c_int32 * 2)(0, rows)
+    view = fc_kv_view(k.data_ptr(), v.data_ptr(), strides[0], strides[1], _DTYPE[dtype], k.shape[1], k.shape[2], 1,
+                      ctypes.cast(cu, POINTER(c_int32)))
     rc = _lib.fc_quantize_cache(handle, byref(view), cache.ref, None if used is None else used.data_ptr(),
                                 None if out_rows is None else out_rows.data_ptr(), _stream_of(k))
     if rc != FC_OK:
