@@ -877,6 +877,7 @@ class Compressor:
         self.out_v = None
         self.out_idx = None
         self._ws = None
+        self.cache4 = None               # quantize() makes them
         self._m = self._mkey = self._mbuffers = None
 
     def close(self):
@@ -1000,6 +1001,17 @@ class Compressor:
                       m["out_v"][l], m["out_idx"][l], m["cap"], opt, m["ws"], m["ws_bytes"], st)
             if rc != FC_OK:
                 raise FlashCacheError(rc, "fc_select_compact_ex")
+
+    def quantize(self):
+        """After `compress`: every layer's kept rows in 4 bits -> a Cache4 per layer, the same ones on every call, for
+        make_decode_args_ex with the layer's `offsets`.  out_k and out_v are not needed for decoding then."""
+        if self.out_k is None:
+            raise ValueError("compress first")
+        if self.cache4 is None or self.cache4[0].capacity_rows < self.out_k.shape[1]:
+            self.cache4 = [Cache4.empty(self.out_k.shape[1], self.H, self.d, self.dtype, self.device) for _ in range(self.L)]
+        for l in range(self.L):
+            fc_quantize_cache(self.handle, self.out_k[l], self.out_v[l], self.cache4[l], used=self.offsets[l, self.B:])
+        return self.cache4
 
     def compress(self, K_layers, V_layers):
         m, st = self._marshal(K_layers, V_layers), _stream()
