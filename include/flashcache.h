@@ -406,7 +406,8 @@ fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k,
  *             Sums and softmax statistics in fp32; a weight is rounded to fp16 (11 bits) once, beside its row's scale.
  *   window    0: every row is visible.  Else, of a sequence's n rows (kept ones, then the tail), only the last `window`
  *   sinks     and the first `sinks` are; the others are not read (whole tiles of them).
- * Rows without weight (outside the window, or past a sequence's end) may hold anything.  A sequence without rows gives zeros.
+ * Rows without weight (outside the window, or past a sequence's end) may hold anything.  A sequence without rows gives zeros
+ * (a query whose scores are all minus infinity NaN: 0 / 0).
  */
 typedef struct {
   const fc_cache4 *cache4;
@@ -421,7 +422,8 @@ fc_status fc_decode_attention_ex(fc_handle *h, const fc_decode_args *a, const fc
  * Attention of a prefill, or of a chunk of one, with a sliding window and sinks: for every sequence b with n_q queries and
  * n_k keys, query i stands at position p = n_k - n_q + i and
  *     out[i] = Softmax over visible j (q[i] k[j] / sqrt(head_dim)) v[j],   j visible:  j <= p and (j > p - window or j < sinks).
- * window >= n_k: plain causal attention.  A query that sees no key (p < 0) gives zeros.  fp32 scores, statistics and sums;
+ * window >= n_k: plain causal attention.  A query that sees no key (p < 0) gives zeros, one whose scores are all minus
+ * infinity NaN (0 / 0).  fp32 scores, statistics and sums;
  * weights are rounded to dtype before the second product.  A key or value that is not finite reaches the queries that see
  * it and no other.
  *

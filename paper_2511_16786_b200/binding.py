@@ -580,6 +580,13 @@ def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
         raise FlashCacheError(rc, "fc_dequantize_cache")
 
 
+def _check_out(q, out, workspace, tokens: int) -> None:
+    if out.dtype != q.dtype or out.device != q.device or not out.is_contiguous() or out.shape[0] < tokens or out.shape[1:] != q.shape[1:]:
+        raise ValueError("out: contiguous, of q's type, device and heads, with room for %d tokens" % tokens)
+    if workspace.device != q.device:
+        raise ValueError("workspace: on q's device")
+
+
 def make_decode_args_ex(q, cache, offsets, max_rows: int, tail_k=None, tail_v=None, tail_len=None, window: int = 0, sinks: int = 0):
     """-> (arguments, options) of fc_decode_attention_ex.  cache: a Cache4, or (cache_k, cache_v) [rows, H, d]; window 0: every row
     is visible, else the last `window` rows and the first `sinks`.  The rest as make_decode_args.  The arguments hold pointers:
@@ -624,6 +631,7 @@ def fc_decode_workspace_bytes_ex(handle, args, options) -> int:
 
 def fc_decode_attention_ex(handle, args, options, out, workspace) -> None:
     """out: [B, Hq, d] device tensor of the cache's type."""
+    _check_out(args._device, out, workspace, args.batch)
     rc = _lib.fc_decode_attention_ex(handle, byref(args), byref(options), out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                                      _stream_of(args._device))
     if rc != FC_OK:
@@ -660,6 +668,7 @@ def fc_window_workspace_bytes(handle, args) -> int:
 
 def fc_window_attention(handle, args, out, workspace) -> None:
     """out: contiguous [Tq, Hq, d] of q's type."""
+    _check_out(args._device, out, workspace, args.cu_seqlens_q[args.kv.contents.batch])
     rc = _lib.fc_window_attention(handle, byref(args), out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(args._device))
     if rc != FC_OK:
         raise FlashCacheError(rc, "fc_window_attention")

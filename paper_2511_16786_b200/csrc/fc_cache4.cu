@@ -387,6 +387,7 @@ extern "C" fc_status fc_quantize_cache(fc_handle *h, const fc_kv_view *kv, const
     return FC_ERR_INVALID_ARG;
   const int64_t rows = kv->cu_seqlens[kv->batch];
   if (rows < 0 || (!out_rows && rows > cache->capacity_rows)) return FC_ERR_INVALID_ARG;
+  if (rows > 0x7fffffffll - 4096) return FC_ERR_UNSUPPORTED;        // row numbers past the last, in whole blocks, are ints too
   if (rows == 0) return FC_OK;
   CacheParams P = params_of(h, cache);
   P.k = static_cast<const char *>(kv->k);

@@ -415,15 +415,19 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         for (int r = 0; r < NQ; ++r) {
           const float n0 = over_rows(x[r].x) + vexp, n1 = over_rows(x[r].y) + vexp;
           const float t0 = n0 > m[r].x + kTop ? n0 - kReset : m[r].x, t1 = n1 > m[r].y + kTop ? n1 - kReset : m[r].y;
-          const float c0 = m[r].x == t0 ? 1.f : exp2f(m[r].x - t0), c1 = m[r].y == t1 ? 1.f : exp2f(m[r].y - t1);
+          // by half the exponent, twice: scales may grow by 2^165, and weights of 2^50 then become such of 2^-115
+          const float c0 = m[r].x == t0 ? 1.f : exp2f(0.5f * (m[r].x - t0)), c1 = m[r].y == t1 ? 1.f : exp2f(0.5f * (m[r].y - t1));
           m[r] = make_float2(t0, t1);
-          l[r].x *= c0; l[r].y *= c1;
-          omin[r][0].x *= c0; omin[r][0].y *= c1;
-          omin[r][1].x *= c0; omin[r][1].y *= c1;
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            oacc[i][r][0] *= c0; oacc[i][r][1] *= c1;
-            oacc[i][r][2] *= c0; oacc[i][r][3] *= c1;
+          for (int k = 0; k < 2; ++k) {
+            l[r].x *= c0; l[r].y *= c1;
+            omin[r][0].x *= c0; omin[r][0].y *= c1;
+            omin[r][1].x *= c0; omin[r][1].y *= c1;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              oacc[i][r][0] *= c0; oacc[i][r][1] *= c1;
+              oacc[i][r][2] *= c0; oacc[i][r][3] *= c1;
+            }
           }
         }
       }
@@ -720,14 +724,14 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
 #pragma unroll 4
       for (int k = 0, w = warp0; k < parts; ++k, w = w + 1 == kWarps ? 0 : w + 1) {
         const float2 ml = mml[w * kHeads + r], mn = mmin[w * kHeads + r];
-        const float f = exp2f(ml.x - ref), add = lane < 16 ? mn.x : mn.y;
+        const float f = exp2f(0.5f * (ml.x - ref)), add = lane < 16 ? mn.x : mn.y;   // twice, as in `refer`
         const float *src = mo + ((size_t)w * kHeads + r) * S::kStride + C * lane;
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = fmaf(src[c] + add, f, o[c]);
-        ll = fmaf(ml.y, f, ll);
+        for (int c = 0; c < C; ++c) o[c] = fmaf((src[c] + add) * f, f, o[c]);
+        ll = fmaf(ml.y * f, f, ll);
       }
       if (i0 == i1) {
-        const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);    // a NaN sum stays one
+        const float inv = 1.f / ll;                                        // 0 only of scores that are all minus infinity: 0 / 0
         T *out = static_cast<T *>(P.out) + ((size_t)b * P.Hq + (size_t)h * P.G + r) * D + C * lane;
 #pragma unroll
         for (int c = 0; c < C; c += 2) *reinterpret_cast<unsigned *>(out + c) = Mma<T>::pack(o[c] * inv, o[c + 1] * inv);
@@ -780,9 +784,9 @@ k_decode_ex_combine(const __grid_constant__ ExParams P, int width) {
   float l = 0.f;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const float f = exp2_fast(ml[e].x - ref);
+    const float f = exp2_fast(0.5f * (ml[e].x - ref));                     // the root of a result's weight (see `refer`)
     weight[tid + kThreadsC * e] = f;
-    l = fmaf(f, ml[e].y, l);
+    l = fmaf(f * ml[e].y, f, l);
   }
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -793,7 +797,7 @@ k_decode_ex_combine(const __grid_constant__ ExParams P, int width) {
   for (int i = first;;) {
 #pragma unroll
     for (int a = 0; a < kAhead; ++a)
-      if (i + groups * a < cnt) acc = fmaf(v[a], weight[i + groups * a], acc);
+      if (i + groups * a < cnt) acc = fmaf(v[a] * weight[i + groups * a], weight[i + groups * a], acc);
     i += groups * kAhead;
     if (i >= cnt) break;
 #pragma unroll
@@ -804,7 +808,7 @@ k_decode_ex_combine(const __grid_constant__ ExParams P, int width) {
   if (first != 0) return;
   for (int k = 1; k < groups; ++k) acc += part[tid + k * width];
   l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);              // a NaN sum stays one
+  const float inv = 1.f / l;
   static_cast<T *>(P.out)[((size_t)b * P.Hq + hq) * D + blockIdx.y * width + c] = Mma<T>::from_float(acc * inv);
 }
 

@@ -567,7 +567,8 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
     if (ok) ok = mbar::wait_warp(&sh.done[q], 0u);
     if (!ok && lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);
     after_sync();
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);    // a NaN sum stays one
+    // nothing seen: 0; only scores of minus infinity: 0 / 0 (their weights by polynomial are not 0)
+    const float inv = p < 0 ? 0.f : (m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l);
     const size_t slot = (((size_t)w.item * P.splits + w.split) * NT + q) * kTileRows + r;
 #pragma unroll 1
     for (int c = 0; c < D; c += 32) {
@@ -625,7 +626,7 @@ k_window_join(const __grid_constant__ WinParams P) {
       acc[c + 1] = fmaf(x.y, f, acc[c + 1]);
     }
   }
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+  const float inv = w.s.nk - w.s.nq + qi < 0 ? 0.f : 1.f / l;     // 0 / 0 of scores that are all minus infinity
   T *out = static_cast<T *>(P.out) + ((size_t)(w.s.q0 + qi) * P.Hq + w.h * P.G + r % P.G) * D + C * lane;
 #pragma unroll
   for (int c = 0; c < C; c += 2) *reinterpret_cast<unsigned *>(out + c) = Mma<T>::pack(acc[c] * inv, acc[c + 1] * inv);

@@ -202,6 +202,37 @@ def test_weights_and_values_of_unlike_sizes(handle, size_k, size_v, peaked, dtyp
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("apart", [True, False])
+@pytest.mark.parametrize("most", [1, 128 * 40])
+def test_scales_at_both_ends_of_bf16(handle, most, apart):
+    """Rows of equal weight whose values are 2^165 apart: what a row adds to the sum of weights counts, however small its scale."""
+    n, d = 128 * 40, 128
+    g = torch.Generator().manual_seed(6)
+    size = torch.full((n, 1, 1), 1e-13)
+    size[torch.arange(n) >= n // 2 if apart else torch.arange(n) % 64 >= 32] = 8e37
+    k, v = torch.zeros((n, 1, d), dtype=torch.bfloat16).cuda(), ((torch.rand((n, 1, d), generator=g) * 2 - 1) * size).to(torch.bfloat16).cuda()
+    q = torch.randn((1, 4, d), generator=g).to(torch.bfloat16).cuda()
+    cache = fc.Cache4.empty(n, 1, d, torch.bfloat16)
+    fc.fc_quantize_cache(handle, k, v, cache)
+    main = _held(cache.codes_k, cache.params_k, False) + _held(cache.codes_v, cache.params_v, True)
+    want, tol = _definition(q, main, [0, n], None, None, 0, 0, torch.bfloat16, True)
+    _check(_run(handle, q, cache, [0, n], None, None, 0, 0, most=most), want, tol)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_scores_that_are_all_minus_infinity_are_undefined(handle, dtype):
+    """0 / 0 by the definition, for the queries and sequences that see nothing else."""
+    lens, H, G, d = [40, 300, 2], 2, 4, 64
+    q, (k, v), main, offs, _ = _case(lens, None, H, G, d, dtype, False, handle, 8)
+    q.abs_().add_(0.5)
+    k[40:340, 1] = float("-inf")
+    k[340, 0] = float("-inf")
+    got = _run(handle, q, (k, v), offs, None, None, 0, 0).isnan()
+    want = torch.zeros_like(got)
+    want[1, G:] = True
+    assert torch.equal(got, want)
+
+
 def test_bound_of_rows_changes_the_launch_only_and_rows_past_the_cache_are_none(handle):
     lens, H, G, d = [500, 64, 3001], 2, 7, 128
     q, cache, main, offs, tail = _case(lens, None, H, G, d, torch.bfloat16, True, handle, 5)

@@ -133,3 +133,25 @@ def test_prompt_to_tokens(fc):
     assert fc.fc_last_device_status(handle) == 0
     comp.close()
     fc.fc_destroy(handle)
+
+
+def test_outputs_that_do_not_fit_are_refused(fc):
+    """By the binding, before anything is launched."""
+    handle = fc.fc_create(0, 1024)
+    q, k = torch.zeros((6, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros((6, 2, 64), dtype=torch.float16, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    offs = torch.arange(7, device="cuda")
+    window = fc.make_window_args(q, k, k, [0, 6], [0, 6], 4)
+    decode = fc.make_decode_args_ex(q, (k, k), offs, 1)
+    for out, room in ((torch.empty_like(q[:5]), ws), (torch.empty_like(q[:, :3]), ws), (torch.empty_like(q).float(), ws),
+                      (torch.empty((6, 8, 64), dtype=q.dtype, device="cuda")[:, ::2], ws), (torch.empty_like(q, device="cpu"), ws),
+                      (torch.empty_like(q), ws.cpu())):
+        with pytest.raises(ValueError):
+            fc.fc_window_attention(handle, window, out, room)
+        with pytest.raises(ValueError):
+            fc.fc_decode_attention_ex(handle, *decode, out, room)
+    comp = fc.Compressor(1, 2, 64, [0, 6], torch.float16, 0.5)
+    with pytest.raises(ValueError):
+        comp.quantize()
+    comp.close()
+    fc.fc_destroy(handle)

@@ -147,6 +147,25 @@ def test_what_is_not_finite_reaches_who_sees_it_and_no_one_else(handle, d, G, wi
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("nq,nk", [([700], [700]), ([4], [6000])])
+def test_scores_that_are_all_minus_infinity_are_undefined(handle, nq, nk, dtype):
+    """0 / 0 by the definition, for the queries whose window holds such keys only; the others give them no weight."""
+    d, window, g = 128, 300, torch.Generator().manual_seed(9)
+    q = (torch.rand((nq[0], 2, d), generator=g) + 0.5).to(dtype).cuda()
+    k, v = (torch.randn((nk[0], 1, d), generator=g).to(dtype).cuda() for _ in range(2))
+    lo, hi = nk[0] - 650, nk[0] - 2
+    k[lo:hi] = float("-inf")
+    args = fc.make_window_args(q, k, v, [0] + nq, [0] + nk, window, 0)
+    ws = torch.empty(fc.fc_window_workspace_bytes(handle, args), dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    fc.fc_window_attention(handle, args, out, ws)
+    at = torch.arange(nq[0]) + nk[0] - nq[0]
+    want = (at < hi) & (at - window + 1 >= lo)
+    assert torch.equal(out.isnan().cpu(), want[:, None, None].expand(nq[0], 2, d))
+    assert want.any() and not want.all()
+
+
 def test_strided_views_and_rows_past_the_last_key(handle):
     # q, k, v out of one projection; keys behind the last sequence hold NaN
     T, Hq, H, d = 333, 4, 2, 64

@@ -154,3 +154,11 @@ def test_cache4_refusals(handle):
                  (handle, ctypes.byref(view()), None)):
         assert fc._lib.fc_quantize_cache(*args, None, None, None) == INVALID
     assert fc._lib.fc_dequantize_cache(None, ctypes.byref(_cache()), A, A, 0, None, None) == INVALID
+
+
+def test_rows_past_the_last_int_are_refused(handle):
+    cu, cache = (ctypes.c_int32 * 2)(0, (1 << 31) - 1), _cache()
+    view = fc.fc_kv_view(A, A, 256, 128, fc.FC_BF16, 2, 128, 1, ctypes.cast(cu, ctypes.POINTER(ctypes.c_int32)))
+    assert fc._lib.fc_quantize_cache(handle, ctypes.byref(view), ctypes.byref(cache), None, A, None) == UNSUPPORTED
+    cu[1] = 65                                              # more than the cache has, without rows to go to
+    assert fc._lib.fc_quantize_cache(handle, ctypes.byref(view), ctypes.byref(cache), None, None, None) == INVALID
