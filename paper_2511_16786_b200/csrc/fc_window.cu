@@ -1,18 +1,28 @@
 // Attention of a prefill with a sliding window and sinks (fc_window_attention).
 //
 // Query i of a sequence stands at p = n_k - n_q + i and sees the keys j <= p with j > p - window or j < sinks;
-//     out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(c s_j - m),  s = q k,  c = log2(e) / sqrt(d),  m >= max c s - 8.
-// 4 d operations per visible pair and query head: bound by the tensor cores, and next to them by the exponentials (16 a
-// cycle and SM, so a 128 x 128 tile takes 1024 cycles, as long as its two products at d = 128).
+//     out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(c s_j - m),  s = q k,  c = log2(e) / sqrt(d),  m a reference near max c s.
+// 4 d operations per visible pair and query head.  The floor is the tensor cores' time; what bounds the kernel is the way of one
+// tile's scores through it (128 keys at d = 128, in cycles: 2000 from scores to weights, of them 770 + 880 for exponentials, sums and
+// rounding, the rest loads, stores and barriers; 1050 for the products that use them and make the next scores): two such tiles
+// take turns, and the tensor cores have work for 2050 of some 3100 cycles.  32768 tokens of 28 heads over 4 (d = 128, bf16, window
+// 4096): 1.77 ms back to back, where the GPU runs at its power limit, 1.62 ms alone (1020 and 1115 TFLOP/s).
 //
-//  * A block has two tiles of 128 query rows and one stream of key tiles (128 keys) for both.  A row is a query of one head; the
-//    query heads that share a KV head lie side by side in a tile (128 / G queries each), so keys are read once for all of
-//    them and a tile spans few positions: little of a short window is masked away.
+//  * Queries are taken in tiles of 128 rows, two to a block that share one stream of key tiles (128 keys).  A row is a query of one
+//    head; the query heads that share a KV head lie side by side in a tile (128 / G queries each), so keys are read once for
+//    all of them and a tile spans few positions: little of a short window is masked away.
 //  * Both products run on tcgen05: scores S = Q K^T from shared memory, outputs O += P V with the weights P (16 bits, written over
-//    the scores they came from) out of tensor memory.  Two times (128 + d) columns hold S and O of both tiles.
-//  * Four warps per tile turn scores into weights, a thread a row; one warp loads (TMA, a ring of key and value tiles), one
-//    issues the products, in an order that works on one tile's products while the other tile's weights are made.
-//  * The reference m moves only when a score passes it by 8 (weights stay below 2^8), so the outputs are rarely rescaled.
+//    the scores they came from) out of tensor memory.  Two times (128 + d) columns hold S and O of both tiles.  Products are issued
+//    in steps of 16 keys; those that no row of the tile sees are left out.
+//  * Four warps per tile turn scores into weights, a thread a row (two threads a row: 1930 us, the barriers between them cost more
+//    than the shorter way gains); one warp loads (TMA, a ring of key and value tiles), one issues the products, in an order
+//    that works on one tile's products while the other tile's weights are made.  O += P V starts on the first 64 keys' weights.
+//  * A quarter of the exponentials (an eighth at d = 64) are polynomials: the special-function units give 16 a cycle and SM, so a
+//    128 x 128 tile would take 1024 cycles, as long as its two products at d = 128 (1770 us; an eighth 1797, three eighths 1807; at
+//    d = 64 a ragged batch 41.3 us with an eighth, 42.4 with a quarter).
+//  * The reference m moves only when a score passes it by 14 (fp16) or 24 (bf16), so the outputs are rarely rescaled, and weights stay
+//    finite.  At d = 128 that none did is read off the sums of the weights; the largest score is only looked for where one did,
+//    in a row's first tile and in tiles seen in part (1807 -> 1773 us; at d = 64, where most tiles are such, 42 -> 46 us).
 //  * Values that are not finite: a product takes 0 x NaN from keys that a row does not see.  Tiles that some row sees in part
 //    are looked through by two more warps, which clear what is not finite and note the keys; rows that see such a key then
 //    add weight x value by themselves.  (Tiles seen by every row need nothing; nor do keys, whose scores are masked.)
@@ -37,6 +47,7 @@ constexpr int kSplitMin = 4;                   // key tiles that a part of a spl
 // How far, in powers of two, a score may pass its row's reference before that moves (and the outputs are rescaled): weights stay
 // below 2^14 in fp16, 2^24 in bf16, and one below 2^-24 of the reference's is nothing in either.
 template <typename T> constexpr float kSlack = std::is_same<T, __half>::value ? 14.f : 24.f;
+template <typename T> constexpr float kMost = std::is_same<T, __half>::value ? 0x1p14f : 0x1p24f;
 
 struct WinSeq { int q0, nq, k0, nk, item; };   // item: first of the sequence's, in blocks before splitting
 
@@ -56,7 +67,7 @@ struct WinParams {
 struct WinMaps { CUtensorMap q, k, v; };
 
 // NT query tiles to a block: two where they share what they read (128 channels); one, and two blocks to an SM, where there is room
-// for it (64): a block's beginning and end then have another's products beside them (the ragged batch of 64 channels, FIXME).
+// for it (64): a block's beginning and end then have another's products beside them (a ragged batch of 64 channels 47 -> 43 us).
 template <int D>
 struct WinShape {
   static constexpr int NT = D == 128 ? 2 : 1;
@@ -73,7 +84,7 @@ struct WinShape {
 
 template <int SLOTS>
 struct WinShared {
-  unsigned long long qfull, full[SLOTS], empty[SLOTS], scores[2], weights[2][2], done[2];      // weights: of the first and the last 64 keys
+  unsigned long long qfull, full[SLOTS], empty[SLOTS], scores[2], weights[2][2], halved[2], done[2];      // weights: of the first and the last 64 keys
   // by value tile, not by slot (an odd ring holds keys and values by turns in one slot): no more than kValues of them are in it
   unsigned long long clean[kValues];
   unsigned bad[kValues][4];                    // keys of the value tile with something not finite
@@ -133,12 +144,24 @@ __device__ __forceinline__ void mma_ts(unsigned lead, unsigned d, unsigned a, un
                ::"r"(lead), "r"(d), "r"(a), "r"(blo), "r"(bhi), "r"(idesc), "r"(add) : "memory");
 }
 
+// The largest; NaN if any is.
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // Two powers of two without the special-function units, which give 16 a cycle and SM and are what the weights wait for: the
 // nearest whole number into the exponent, the rest (at most half) by the polynomial of degree 4 with the smallest largest relative
 // error on [-1/2, 1/2] (2.7e-6, found by linear programming over 4001 points).  From -126 on down it stays at 2^-126, so it is
-// for tiles without masked scores; NaN is not kept.
+// for tiles without masked scores; NaN becomes something above 2^127.
 __device__ __forceinline__ float2 exp2_poly(float2 x) {
-  x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+  x = make_float2(max_nan(x.x, -126.f), max_nan(x.y, -126.f));
   const float2 r = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));                     // 1.5 * 2^23: the last bits are the number
   const float2 n = __fadd2_rn(r, make_float2(-12582912.f, -12582912.f));
   const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
@@ -149,13 +172,6 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
   p = __ffma2_rn(p, f, make_float2(0.9999992251396179f, 0.9999992251396179f));
   return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(r.x) << 23)),
                      __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(r.y) << 23)));
-}
-
-// The largest; NaN if any is.
-__device__ __forceinline__ float max_nan(float a, float b, float c) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -272,7 +288,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
     mbar::init(&sh.qfull, 1u);
     for (int i = 0; i < kSlots; ++i) { mbar::init(&sh.full[i], 1u); mbar::init(&sh.empty[i], 1u); }
     for (int i = 0; i < kValues; ++i) mbar::init(&sh.clean[i], 2u);
-    for (int q = 0; q < 2; ++q) { mbar::init(&sh.scores[q], 1u); mbar::init(&sh.weights[q][0], 4u); mbar::init(&sh.weights[q][1], 4u); mbar::init(&sh.done[q], 1u); }
+    for (int q = 0; q < 2; ++q) { mbar::init(&sh.scores[q], 1u); mbar::init(&sh.halved[q], 1u); mbar::init(&sh.weights[q][0], 4u); mbar::init(&sh.weights[q][1], 4u); mbar::init(&sh.done[q], 1u); }
     mbar::init_done();
   }
   if (warp == kLoads && lane == 0) { prefetch_map(&M.q); prefetch_map(&M.k); prefetch_map(&M.v); }
@@ -321,6 +337,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       const unsigned qb = (umma::smem_addr(smem) >> 4) | umma::operand_lo(16);
       const unsigned kb = (umma::smem_addr(ring) >> 4) | umma::operand_lo(16), vb = (umma::smem_addr(ring) >> 4) | umma::operand_lo(S::kBox);
       unsigned turn[2] = {0u, 0u};
+      const WinItem w = item;                                      // in registers
       auto scores = [&](int q, int i) {                            // S of tile q with keys i of the ring
         const unsigned k = kb + (unsigned)((2 * i) % kSlots) * (S::kTileBytes / 16), a = qb + (unsigned)q * (S::kTileBytes / 16);
 #pragma unroll
@@ -343,9 +360,11 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         const int kt = w.key_tile(w.u0 + i), vi = 2 * i + 1, vs = vi % kSlots, ki = vi + 1;
         const bool next = i + 1 < n;
         const int kn = next ? w.key_tile(w.u0 + i + 1) : 0;
-        if (!mbar::wait_warp(&sh.clean[i % kValues], (unsigned)(i / kValues) & 1u)) { ok = false; break; }
+        if (!mbar::wait_warp(&sh.full[vs], (unsigned)(vi / kSlots) & 1u) ||
+            (next && !mbar::wait_warp(&sh.full[ki % kSlots], (unsigned)(ki / kSlots) & 1u))) { ok = false; break; }
 #pragma unroll
         for (int q = 0; q < NT && ok; ++q) {
+          if (q == NT - 1 && !mbar::wait_warp(&sh.clean[i % kValues], (unsigned)(i / kValues) & 1u)) { ok = false; break; }
           if (sees_some(P, w.at[q], kt)) {
             const unsigned steps = seen_steps(P, w.at[q], kt);
 #pragma unroll
@@ -355,16 +374,13 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
               for (int c = 4 * half; c < 4 * half + 4; ++c)
                 if ((steps >> c) & 1u) mma_ts(lead, tmem + 128u * (NT + q), tmem + 128u * q + 8u * c, vb + (unsigned)vs * (S::kTileBytes / 16) + 128u * c, hi, o_desc, 1u);
+              if (half == 0) umma::commit(lead, &sh.halved[q]);
             }
             if (!ok) break;
             ++turn[q];
           }
           if (q == NT - 1) umma::commit(lead, &sh.empty[vs]);
           if (next) {
-            if (q == 0) {
-              if (!mbar::wait_warp(&sh.full[ki % kSlots], (unsigned)(ki / kSlots) & 1u)) { ok = false; break; }
-              after_sync();
-            }
             if (sees_some(P, w.at[q], kn)) scores(q, i + 1);
             if (q == NT - 1) umma::commit(lead, &sh.empty[ki % kSlots]);
           }
@@ -446,6 +462,51 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
       for (int c = 0; c < 128; c += 32) tm_ld32(s_at + c, s + c);
       tm_wait_ld(s);
+      float2 sum;
+      unsigned pk[32];
+      auto weights = [&](int c, float ref) {                       // of the keys c .. c + 63, all seen by all
+        const float2 minus = make_float2(-ref, -ref);
+        sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float2 x = __ffma2_rn(make_float2(s[c + 2 * j], s[c + 2 * j + 1]), scale, minus);
+          const float2 y = (j & (D == 128 ? 3 : 7)) == 3 ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          sum = __fadd2_rn(sum, y);
+          pk[j] = Mma<T>::pack(y.x, y.y);
+        }
+      };
+      auto ready = [&](int half) {
+        before_sync();
+        __syncwarp();
+        if (lane == 0) mbar::arrive(&sh.weights[q][half]);
+      };
+      auto give = [&](int half) {
+        tm_st32(s_at + 32 * half, pk);
+        tm_wait_st();
+        ready(half);
+        l += sum.x + sum.y;
+      };
+      // As a rule the reference stays as it is, and that it may shows in the sums: a weight that passes its bound makes a sum that does
+      // (so does NaN).  No largest score is looked for then.
+      const bool quick = D == 128 && !looked && turn > 1u && !__any_sync(0xffffffffu, have && m == -INFINITY);
+      bool begun = false;                                          // the first half is the product's already
+      if (quick) {
+        const float ref = m == -INFINITY ? 0.f : m;
+        auto fits = [&]() { return !__any_sync(0xffffffffu, have && !(sum.x + sum.y <= kMost<T>)); };
+        weights(0, ref);
+        if (fits()) {
+          give(0);
+          weights(64, ref);
+          if (fits()) {
+            give(1);
+            continue;
+          }
+          begun = true;
+          if (ok) ok = mbar::wait_warp(&sh.halved[q], (turn - 1u) & 1u);
+          if (!ok) break;
+          after_sync();
+        }
+      }
       unsigned chunks = 0u;                                        // of a tile seen in part: 32 keys at a time, those that a row of the warp sees
       float top;                                                   // NaN if any score is
       if (all) {
@@ -474,7 +535,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         }
       }
       top *= P.scale_log2;
-      const bool move = top > m + kSlack<T>;
+      const bool move = top > m + (quick ? kSlack<T> - 7.f : kSlack<T>);          // a sum of 64 has passed it
       if (__any_sync(0xffffffffu, move)) {
         const float to = move ? top : m, f = m == to ? 1.f : exp2f(m - to);
         m = to;
@@ -492,32 +553,16 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         }
       }
       const float ref = top != top ? top : (m == -INFINITY ? 0.f : m);                       // a NaN among the scores: all weights
-      const float2 minus = make_float2(-ref, -ref);
-      float2 sum = make_float2(0.f, 0.f);
-      auto weights = [&](int c) {                                  // of the keys c .. c + 63, all seen by all
-        unsigned pk[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float2 x = __ffma2_rn(make_float2(s[c + 2 * j], s[c + 2 * j + 1]), scale, minus);
-          const float2 y = (j & 3) == 3 ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
-          sum = __fadd2_rn(sum, y);
-          pk[j] = Mma<T>::pack(y.x, y.y);
-        }
-        tm_st32(s_at + c / 2, pk);
-      };
-      auto ready = [&](int half) {
-        before_sync();
-        __syncwarp();
-        if (lane == 0) mbar::arrive(&sh.weights[q][half]);
-      };
       if (!looked) {                                               // the product starts on half of them
-        weights(0);
-        tm_wait_st();
-        ready(0);
-        weights(64);
-        tm_wait_st();
-        ready(1);
+        if (!begun) {
+          weights(0, ref);
+          give(0);
+        }
+        weights(64, ref);
+        give(1);
       } else {
+        const float2 minus = make_float2(-ref, -ref);
+        sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           unsigned pk[16];
@@ -561,8 +606,8 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         }
         ready(0);
         ready(1);
+        l += sum.x + sum.y;
       }
-      l += sum.x + sum.y;
     }
     if (ok) ok = mbar::wait_warp(&sh.done[q], 0u);
     if (!ok && lane == 0) atomicOr(P.status, FC_DEV_FLAG_TIMEOUT);

@@ -219,6 +219,7 @@ def test_scales_at_both_ends_of_bf16(handle, most, apart):
     _check(_run(handle, q, cache, [0, n], None, None, 0, 0, most=most), want, tol)
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_scores_that_are_all_minus_infinity_are_undefined(handle, dtype):
     """0 / 0 by the definition, for the queries and sequences that see nothing else."""
@@ -233,6 +234,7 @@ def test_scores_that_are_all_minus_infinity_are_undefined(handle, dtype):
     assert torch.equal(got, want)
 
 
+@pytest.mark.gpu
 def test_bound_of_rows_changes_the_launch_only_and_rows_past_the_cache_are_none(handle):
     lens, H, G, d = [500, 64, 3001], 2, 7, 128
     q, cache, main, offs, tail = _case(lens, None, H, G, d, torch.bfloat16, True, handle, 5)

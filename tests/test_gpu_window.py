@@ -148,6 +148,29 @@ def test_what_is_not_finite_reaches_who_sees_it_and_no_one_else(handle, d, G, wi
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at,much", [((130,), 60.0), ((200,), 60.0), ((263, 391), 40.0), ((130, 131, 250, 255, 400), 25.0), ((640, 700), 300.0),
+                                     ((134,), math.nan), ((201,), math.nan), ((255,), math.nan), ((128,), -math.inf)])
+def test_single_keys_far_above_the_rest(handle, at, much, d, dtype):
+    """In either half of a tile that all queries see whole: the reference moves in the middle of a tile, and NaN is seen
+    wherever it stands.  `much`: how many powers of two such a key's weight is above the others'; every second head turns away."""
+    nq, nk, g = 70, 900, torch.Generator().manual_seed(int(sum(at)))
+    base = torch.randn(d, generator=g)
+    q = base + 0.1 * torch.randn((nq, 2, d), generator=g)
+    q[:, 1] *= -1
+    k, v = (0.3 * torch.randn((nk, 1, d), generator=g) for _ in range(2))
+    for i, key in enumerate(at):
+        k[key] = base / (base @ base) * much * (1 + i / 4) * math.sqrt(d) * math.log(2.0) if math.isfinite(much) else much
+    q, k, v = (x.to(dtype).cuda() for x in (q, k, v))
+    out, (want, tol) = _run(handle, q, k, v, [nq], [nk], 5000, 0), _definition(q, k, v, [nq], [nk], 5000, 0)
+    if math.isfinite(much):
+        _check(out, want, tol)
+    else:
+        assert want.isnan().all() and out.isnan().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("nq,nk", [([700], [700]), ([4], [6000])])
 def test_scores_that_are_all_minus_infinity_are_undefined(handle, nq, nk, dtype):
     """0 / 0 by the definition, for the queries whose window holds such keys only; the others give them no weight."""
@@ -166,6 +189,7 @@ def test_scores_that_are_all_minus_infinity_are_undefined(handle, nq, nk, dtype)
     assert want.any() and not want.all()
 
 
+@pytest.mark.gpu
 def test_strided_views_and_rows_past_the_last_key(handle):
     # q, k, v out of one projection; keys behind the last sequence hold NaN
     T, Hq, H, d = 333, 4, 2, 64
