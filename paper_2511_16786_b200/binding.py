@@ -495,25 +495,22 @@ def fc_decode_attention(handle, args, out, workspace) -> None:
 def _stream_of(t: torch.Tensor) -> int:
     """The current stream of the device that `t` lives on, which need not be the current device."""
     if _raw_stream is not None:
-        return _raw_stream(t.device.index)
+        return _raw_stream(t.get_device())
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _same_device(first, *others) -> None:
-    at = None
-    for t in (first, *others):
-        if t is not None:
-            if at is None:
-                at = t.device
-                if at.type != "cuda":
-                    raise ValueError("tensors of one CUDA device: got %s" % at)
-            elif t.device != at:
-                raise ValueError("tensors of one CUDA device: got %s and %s" % (at, t.device))
+    at = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != at:
+            raise ValueError("tensors of one CUDA device: got %s and %s" % (first.device, t.device))
+    if at < 0:
+        raise ValueError("tensors of one CUDA device: got %s" % first.device)
 
 
-def _counter(t, what: str, numel: int | None = None) -> None:
-    if t is not None and (t.dtype != torch.int64 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
-        raise ValueError("%s: contiguous int64 device tensor%s" % (what, "" if numel is None else " of %d" % numel))
+def _counter(t, what: str, numel: int) -> None:
+    if t.dtype != torch.int64 or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError("%s: contiguous int64 device tensor of %d" % (what, numel))
 
 
 class Cache4:
@@ -547,18 +544,22 @@ class Cache4:
         return sum(t.nbytes for t in (self.codes_k, self.codes_v, self.params_k, self.params_v))
 
 
+_two_ints = c_int32 * 2
+
+
 def fc_quantize_cache(handle, k, v, cache: Cache4, used=None, out_rows=None) -> None:
     """Rows k, v [rows, H, d] into 4 bits.  used: int64 [1] on the device, how many of them; out_rows: int64 [rows] on the device,
     the cache row each goes to (negative: left out)."""
-    rows, strides, dtype = k.shape[0], k.stride(), k.dtype
-    if k.dim() != 3 or v.shape != k.shape or v.dtype != dtype or v.stride() != strides or strides[2] != 1 or dtype not in _DTYPE:
+    shape, strides, dtype = k.shape, k.stride(), k.dtype
+    if len(shape) != 3 or v.shape != shape or v.dtype != dtype or v.stride() != strides or strides[2] != 1 or dtype not in _DTYPE:
         raise ValueError("k and v: [rows, H, d] of one dtype, laid out alike, channel stride 1")
+    rows, heads, d = shape
     _same_device(k, v, cache.codes_k, used, out_rows)
-    _counter(used, "used", 1)
-    _counter(out_rows, "out_rows", rows)
-    cu = (c_int32 * 2)(0, rows)
-    view = fc_kv_view(k.data_ptr(), v.data_ptr(), strides[0], strides[1], _DTYPE[dtype], k.shape[1], k.shape[2], 1,
-                      ctypes.cast(cu, POINTER(c_int32)))
+    if used is not None:
+        _counter(used, "used", 1)
+    if out_rows is not None:
+        _counter(out_rows, "out_rows", rows)
+    view = fc_kv_view(k.data_ptr(), v.data_ptr(), strides[0], strides[1], _DTYPE[dtype], heads, d, 1, _two_ints(0, rows))
     rc = _lib.fc_quantize_cache(handle, byref(view), cache.ref, None if used is None else used.data_ptr(),
                                 None if out_rows is None else out_rows.data_ptr(), _stream_of(k))
     if rc != FC_OK:
@@ -567,13 +568,14 @@ def fc_quantize_cache(handle, k, v, cache: Cache4, used=None, out_rows=None) -> 
 
 def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
     """The values the first rows of the cache stand for into out_k, out_v [rows, H, d] (`used`: as in fc_quantize_cache)."""
-    rows = out_k.shape[0]
-    shape = (rows, cache.num_heads, cache.head_dim)
-    for o in (out_k, out_v):
-        if o.shape != shape or o.dtype != cache.dtype or not o.is_contiguous():
-            raise ValueError("out_k/out_v: contiguous [rows, H, d] of the cache's type")
+    shape, dtype = out_k.shape, cache.dtype
+    rows = shape[0]
+    if (shape != (rows, cache.num_heads, cache.head_dim) or out_v.shape != shape or out_k.dtype != dtype or out_v.dtype != dtype
+            or not out_k.is_contiguous() or not out_v.is_contiguous()):
+        raise ValueError("out_k/out_v: contiguous [rows, H, d] of the cache's type")
     _same_device(out_k, out_v, cache.codes_k, used)
-    _counter(used, "used", 1)
+    if used is not None:
+        _counter(used, "used", 1)
     rc = _lib.fc_dequantize_cache(handle, cache.ref, out_k.data_ptr(), out_v.data_ptr(), rows, None if used is None else used.data_ptr(),
                                   _stream_of(out_k))
     if rc != FC_OK:
@@ -581,9 +583,11 @@ def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
 
 
 def _check_out(q, out, workspace, tokens: int) -> None:
-    if out.dtype != q.dtype or out.device != q.device or not out.is_contiguous() or out.shape[0] < tokens or out.shape[1:] != q.shape[1:]:
+    at, shape = q.get_device(), out.shape
+    if (out.dtype != q.dtype or out.get_device() != at or not out.is_contiguous()
+            or (shape != q.shape and (shape[0] < tokens or shape[1:] != q.shape[1:]))):
         raise ValueError("out: contiguous, of q's type, device and heads, with room for %d tokens" % tokens)
-    if workspace.device != q.device:
+    if workspace.get_device() != at:
         raise ValueError("workspace: on q's device")
 
 
