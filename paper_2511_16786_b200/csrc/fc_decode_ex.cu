@@ -1,19 +1,22 @@
 // Decoding step over rows held in 4 bits or in 16, with or without a window and sinks (fc_decode_attention_ex).
 //
 // For every sequence and query head  out = sum_j w_j v_j / sum_j w_j,  w_j = exp(q k_j / sqrt d)  over the visible rows j: kept
-// rows, then the 16-bit tail.  A step reads every visible row once and is bound by that read, so the frame is that of
-// fc_decode.cu: the tiles of all sequences and heads form one line, one block per SM takes an equal share of it, a warp
-// keeps a ring of tiles in flight, the other warps only ever wait for the tile they use, blocks that share a sequence meet
-// in a second kernel.  What differs:
+// rows, then the 16-bit tail.  A step reads every visible row once; the frame is that of fc_decode.cu: the tiles of all
+// sequences and heads form one line, one block per SM takes an equal share of it, a warp keeps a ring of tiles in flight, the
+// other warps only ever wait for the tile they use, blocks that share a sequence meet in a second kernel.
+// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 34 us, 3.2 TB/s; 41769 rows of 32 heads 49.5 us, 3.9 TB/s: some
+// 7 us for two launches, the first tile and the joins, the rest bound by the instructions (0.53 a cycle and scheduler, over the
+// whole kernel; a 4-bit row has 3.6 times the arithmetic per byte of a 16-bit one).  A step over 820 rows takes 7.3 us.
 //
-//  * A row of 4 bits is 72 bytes of K or V at d = 128 instead of 256, so the arithmetic per byte is 3.6 times that of 16-bit
-//    rows and the instructions per row, not the bytes, are what could run out.  Nothing is expanded in memory or to fp32:
+//  * A row of 4 bits is 72 bytes of K or V at d = 128 instead of 256.  Nothing is expanded in memory or to fp32:
 //    - codes are masked out of the loaded words and are the tensor cores' operands as they stand, as subnormal half numbers
 //      (code * 2^-24, exact; the second nibble of a word is 16 times that, which the queries or the output rows undo);
-//    - a half row's scale multiplies sums of 32 products (keys) or the weights (values), never a code;
+//    - a half row's scale multiplies sums of d/2 products (keys) or the weights (values), never a code;
 //    - its minimum goes with the sum of the query's channels (keys) or with a sum of weights (values), both in fp32.
-//    Scores take queries as the products' rows; outputs are kept turned round, channels as rows and queries as columns, since
-//    the scores' accumulator is then the second product's operand in place, and eight columns are enough for 8 query heads.
+//    Rows of the cache are the rows of the first product and queries its columns, channels the rows of the second: the scores,
+//    turned round in registers (8 x 8 blocks, one instruction each), are the second product's right operand, what a lane keeps
+//    of a query stays with it, and eight columns are enough for 8 query heads (queries as rows: 43 and 61 us).
+//  * Four warps share a tile of 128 rows, 32 each, and three such teams take the tiles by turns (two: 43 and 66 us, queries as rows).
 //  * Queries are brought to 2^14 .. 2^15 by a power of two before they become half numbers (exact but for channels 2^-25 of the
 //    largest); weights are kept below 2^15 together with the largest scale met so far, so rounding them to half numbers (11 bits)
 //    neither overflows nor loses the small ones, whatever the range of the cache's type.

@@ -155,3 +155,84 @@ def test_outputs_that_do_not_fit_are_refused(fc):
         comp.quantize()
     comp.close()
     fc.fc_destroy(handle)
+
+
+def test_offsets_past_32_bits(fc):
+    """Rows far into a cache of 4.6 GB, and tokens far apart in one of 5 GB."""
+    handle = fc.fc_create(0, 1024)
+    g = torch.Generator().manual_seed(3)
+    n, Hn, d, cap = 300, 32, 128, 2_250_000
+    k, v = (torch.randn((n, Hn, d), generator=g).to(torch.float16).cuda() for _ in range(2))
+    q = torch.randn((1, Hn, d), generator=g).to(torch.float16).cuda()
+    outs = []
+    for rows, first in ((n, 0), (cap, cap - n)):
+        cache = fc.Cache4.empty(rows, Hn, d, torch.float16)
+        to = torch.arange(first, first + n, device="cuda")
+        fc.fc_quantize_cache(handle, k, v, cache, out_rows=to)
+        dec = fc.make_decode_args_ex(q, cache, torch.tensor([first, first + n], device="cuda"), n)
+        ws = torch.empty(fc.fc_decode_workspace_bytes_ex(handle, *dec), dtype=torch.uint8, device="cuda")
+        outs.append(torch.empty_like(q))
+        fc.fc_decode_attention_ex(handle, *dec, outs[-1], ws)
+        assert fc.fc_last_device_status(handle) == 0
+        del cache
+    assert torch.equal(outs[0], outs[1]) and bool(outs[0].any())
+    far = torch.empty(n * 2 ** 23, dtype=torch.float16, device="cuda")
+    kv = [far.as_strided((n, Hn, d), (2 ** 23, d, 1), i * Hn * d) for i in range(3)]           # keys, values, queries
+    for x, y in zip(kv, (k, v, k + v)):
+        x.copy_(y)
+    freq, _ = fc.fc_rotary_frequencies(d)
+    pos = torch.arange(n, device="cuda")
+    outs = []
+    for kk, vv, qq in (kv, (k.clone(), v, k + v)):
+        fc.fc_rotary(handle, fc.make_rotary_args(pos, freq, q=qq, out_q=qq, k=kk, out_k=kk))
+        args = fc.make_window_args(qq, kk, vv, [0, n], [0, n], 90, 2)
+        ws = torch.empty(fc.fc_window_workspace_bytes(handle, args), dtype=torch.uint8, device="cuda")
+        outs.append(torch.empty((n, Hn, d), dtype=torch.float16, device="cuda"))
+        fc.fc_window_attention(handle, args, outs[-1], ws)
+    assert torch.equal(outs[0], outs[1]) and bool(outs[0].isfinite().all())
+    assert fc.fc_last_device_status(handle) == 0
+    fc.fc_destroy(handle)
+
+
+def test_two_handles_on_two_streams_at_once(fc):
+    import threading
+
+    d, Hn, n = 128, 4, 900
+    g = torch.Generator().manual_seed(12)
+    data = [[torch.randn((n, heads, d), generator=g).to(torch.bfloat16).cuda() for heads in (8, Hn, Hn)] for _ in range(2)]
+    torch.cuda.synchronize()
+
+    def chain(q, k, v, times):
+        handle = fc.fc_create(0, 1024)
+        cache = fc.Cache4.empty(n, Hn, d, torch.bfloat16)
+        args = fc.make_window_args(q, k, v, [0, n], [0, n], 200, 4)
+        offs = torch.tensor([0, 500, 500, n], device="cuda")
+        dec = fc.make_decode_args_ex(q[:3].contiguous(), cache, offs, n)
+        wa = torch.empty(fc.fc_window_workspace_bytes(handle, args), dtype=torch.uint8, device="cuda")
+        wd = torch.empty(fc.fc_decode_workspace_bytes_ex(handle, *dec), dtype=torch.uint8, device="cuda")
+        seen = []
+        for _ in range(times):
+            a, b = torch.empty_like(q), torch.empty_like(q[:3])
+            fc.fc_window_attention(handle, args, a, wa)
+            fc.fc_quantize_cache(handle, k, v, cache)
+            fc.fc_decode_attention_ex(handle, *dec, b, wd)
+            seen.append((a, b))
+        assert fc.fc_last_device_status(handle) == 0
+        fc.fc_destroy(handle)
+        return seen
+
+    want = [chain(*x, 1)[0] for x in data]
+    got = [None, None]
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got[i] = chain(*data[i], 30)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(2):
+        for a, b in got[i]:
+            assert torch.equal(a, want[i][0]) and torch.equal(b, want[i][1])
