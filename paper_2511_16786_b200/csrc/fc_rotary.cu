@@ -5,7 +5,7 @@
 // The path reads and writes every row once and computes next to nothing: it is bound by HBM (or, for a step's few rows, by
 // one launch).  So a block takes whole tokens: the angles of a token are computed once, by one thread per pair, and all
 // heads use them from shared memory; every thread then moves 32 bytes of a row (16 of either member of its pairs).
-// 32768 tokens of 28 + 4 heads of 128 (bf16): 94.5 us, 5.7 TB/s; a step's 8 tokens 2.8 us.
+// 32768 tokens of 28 + 4 heads of 128 (bf16): 86.5 us, 6.2 TB/s, 0.95 of a plain copy; a step's 8 tokens 2.6 us.
 // Angles: p f in turns, in 64 bits and the remainder of the frequency's rounding, reduced by whole turns before anything is
 // rounded to 32 (at p = 10^6 a product in 32 bits is off by 0.06 radians); sine and cosine of the remainder by sincospif.
 #include "fc_common.cuh"
@@ -47,7 +47,9 @@ template <typename T, int V> struct alignas(sizeof(T) * V) RotVec { T x[V]; };
 template <typename T, int V, bool INTER>
 __global__ void __launch_bounds__(kRotThreads)
 k_rotary(const __grid_constant__ RotParams P, int tokens_per_block) {
-  extern __shared__ float2 cs[];                     // [token][pair]
+  // [token][pair], the pairs of a thread 16 bytes at a time beside those of its neighbours (94.7 -> 90.6 us: in a run of its own each
+  // thread's pairs meet its neighbours' in the same banks; the rest of the way to 86.5 are divisions)
+  extern __shared__ __align__(16) float2 cs[];
   using Vec = RotVec<T, V>;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   const long long t0 = (long long)blockIdx.x * tokens_per_block;
@@ -55,20 +57,24 @@ k_rotary(const __grid_constant__ RotParams P, int tokens_per_block) {
   const int pairs = P.R / 2;
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   for (int i = threadIdx.x; i < nt * pairs; i += kRotThreads) {
-    const int t = i / pairs, j = i - t * pairs;
+    const int t = (int)((unsigned)i / (unsigned)pairs), j = i - t * pairs;
     const int axis = j < P.end1 ? 0 : (j < P.end2 ? 1 : 2);
     const double p = (double)P.pos[axis * P.pos_axis + t0 + t];
     double turn = fma(p, P.turns[j], -rint(p * P.turns[j])) + p * P.more[j];
     turn -= rint(turn);
     float s, c;
     sincospif(2.f * (float)turn, &s, &c);
-    cs[i] = make_float2(c * P.scale, s * P.scale * P.sign);
+    const int at = V == 1 ? j : 2 * ((j % V) / 2 * (pairs / V) + j / V) + (j & 1);
+    cs[t * pairs + at] = make_float2(c * P.scale, s * P.scale * P.sign);
   }
   __syncthreads();
+  // r / per_head is the high word of r * over: exact, r * per_head stays below 2^32 (12288 heads of 512)
+  const unsigned over = 0xffffffffu / (unsigned)(P.d / (2 * V)) + 1u;
   const int per_head = P.d / (2 * V), per_token = (P.Hq + P.H + P.Hv) * per_head, turned = pairs / V;
   for (int i = threadIdx.x; i < nt * per_token; i += kRotThreads) {
-    const int t = i / per_token, r = i - t * per_token;
-    int h = r / per_head;
+    int t = 0, r = i;
+    while (r >= per_token) { r -= per_token; ++t; }  // a token or two
+    int h = (int)__umulhi((unsigned)r, over);
     const int e = r - h * per_head;
     const char *src;
     char *dst;
@@ -98,7 +104,16 @@ k_rotary(const __grid_constant__ RotParams P, int tokens_per_block) {
     const Vec a = *reinterpret_cast<const Vec *>(src + c0 * sizeof(T)), b = *reinterpret_cast<const Vec *>(src + c1 * sizeof(T));
     Vec x = a, y = b;
     if (!copy) {
-      const float2 *w = cs + t * pairs + V * e;
+      float2 w[V];
+      if constexpr (V == 1) w[0] = cs[t * pairs + e];
+      else {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+          const float4 two = reinterpret_cast<const float4 *>(cs + t * pairs)[j / 2 * turned + e];
+          w[j] = make_float2(two.x, two.y);
+          w[j + 1] = make_float2(two.z, two.w);
+        }
+      }
       if (INTER) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -127,8 +142,8 @@ template <typename T>
 fc_status launch_rotary(fc_handle *h, const RotParams &P, bool inter, cudaStream_t st) {
   constexpr int W = 16 / (int)sizeof(T);
   const bool wide = P.R % (2 * W) == 0;
-  // Two tokens to a block where the blocks come in many waves (32768 tokens of 32 heads 102 -> 94 us, 4 and 8 tokens 94 and 100),
-  // else one (5001 tokens of 64 heads 28 us; 29, 33 and 47 with 2, 4 and 8: fewer blocks fill the last wave worse).
+  // Two tokens to a block where the blocks come in many waves (32768 tokens of 32 heads 94 -> 86 us, 4 tokens 87), else one (5001
+  // tokens of 64 heads 27.4 us; 29 and 32 with 2 and 4: fewer blocks fill the last wave worse).
   const int tb = P.T > 64ll * h->num_sms ? 2 : 1;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((P.T + tb - 1) / tb));
