@@ -6,7 +6,7 @@
 // candidate with the range, the code by the sign of what is left over beside a tie, in 64 bits where it is close.
 // Every row is read once and written once.  A lane holds 16 consecutive channels (32 bytes), 8 or 4 lanes a row of K and the same
 // row of V; the nibbles change lanes in registers, and every lane writes 8 bytes of codes.  16384 rows of 32 heads: 82 us, 4.2 TB/s,
-// bound by the instructions (about 16 a value; 8 channels to a lane 131 us); back 73 us, 4.7 TB/s.
+// bound by the instructions (about 16 a value; 8 channels to a lane 131 us); back 70 us, 4.9 TB/s.
 #include "fc_cache4.cuh"
 
 namespace {
@@ -22,8 +22,7 @@ template <> struct Num<__half> {
   static __device__ __half bits(unsigned short b) { return __ushort_as_half(b); }
   static __device__ unsigned short bits(__half x) { return __half_as_ushort(x); }
   static __device__ float2 both(unsigned w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
-  static __device__ unsigned pack(float a, float b) { const __half2 v = __floats2half2_rn(a, b); return *reinterpret_cast<const unsigned *>(&v); }
-  static constexpr unsigned kNan = 0x7e00u;
+  static constexpr unsigned kNan = 0x7e00u, kUnits = 0x6400u;        // 1024
 };
 template <> struct Num<__nv_bfloat16> {
   using T2 = __nv_bfloat162;
@@ -33,8 +32,7 @@ template <> struct Num<__nv_bfloat16> {
   static __device__ __nv_bfloat16 bits(unsigned short b) { return __ushort_as_bfloat16(b); }
   static __device__ unsigned short bits(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
   static __device__ float2 both(unsigned w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-  static __device__ unsigned pack(float a, float b) { const __nv_bfloat162 v = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const unsigned *>(&v); }
-  static constexpr unsigned kNan = 0x7fc0u;
+  static constexpr unsigned kNan = 0x7fc0u, kUnits = 0x4300u;        // 128
 };
 
 struct CacheParams {
@@ -268,8 +266,6 @@ k_quantize(const CacheParams P, int rounds) {
   }
 }
 
-__device__ __forceinline__ float biased(unsigned x) { return __uint_as_float(0x4b000000u | (x & 15u)); }      // 2^23 + code
-
 template <typename T, int D, bool VALUES>
 __device__ __forceinline__ void values_row(const unsigned char *codes, const char *params, int u, uint4 (&out)[2]) {
   constexpr int HALF = D / 32;
@@ -292,15 +288,24 @@ __device__ __forceinline__ void values_row(const unsigned char *codes, const cha
     word[0] = odd ? got : first;
     word[1] = odd ? second : got;
   }
-  const float2 sl = Num<T>::both(reinterpret_cast<const unsigned *>(params)[u / HALF]);
+  // Two neighbours at a time: their nibbles under the exponent of the first number whose last bit is 1, less that number, are the
+  // codes; what they stand for is one fused operation, and so rounded once.
+  using T2 = typename Num<T>::T2;
+  const T2 sl = reinterpret_cast<const T2 *>(params)[u / HALF];
+  const unsigned one = Num<T>::kUnits | (Num<T>::kUnits << 16);
+  T2 scale, low, units;
+  scale.x = scale.y = sl.x;
+  low.x = low.y = sl.y;
+  units = *reinterpret_cast<const T2 *>(&one);
 #pragma unroll
   for (int a = 0; a < 2; ++a) {
     unsigned r[4];
+    const unsigned next = word[a] >> 4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 c = __fadd2_rn(make_float2(biased(word[a] >> (8 * i)), biased(word[a] >> (8 * i + 4))), make_float2(-8388608.f, -8388608.f));
-      const float2 y = __ffma2_rn(c, make_float2(sl.x, sl.x), make_float2(sl.y, sl.y));
-      r[i] = Num<T>::pack(y.x, y.y);
+      const unsigned x = (__byte_perm(word[a], next, i | ((4 + i) << 8)) & 0x000f000fu) | one;
+      const T2 y = __hfma2(__hsub2(*reinterpret_cast<const T2 *>(&x), units), scale, low);
+      r[i] = *reinterpret_cast<const unsigned *>(&y);
     }
     out[a] = make_uint4(r[0], r[1], r[2], r[3]);
   }
@@ -340,11 +345,13 @@ k_dequantize(const CacheParams P, int rounds) {
   }
 }
 
+// most: rounds of a block, once every SM has its blocks many times over.  Forth the next round's loads are under way beside the
+// arithmetic (16384 rows of 32 heads: 107, 91, 84, 81, 81 and 95 us with 1, 2, 4, 8, 16 and 32); back there is little to hide and many
+// short blocks spread the writes better (71, 70, 72, 77, 89 and 149 us).
 template <typename K>
-fc_status launch_rows(fc_handle *h, K kern, const CacheParams &P, int D, cudaStream_t st) {
+fc_status launch_rows(fc_handle *h, K kern, const CacheParams &P, int D, int most, cudaStream_t st) {
   const long long rows_per_round = kQThreads / (D / 16), rounds_all = (P.rows + rows_per_round - 1) / rows_per_round;
-  // several rounds per block, the next one's loads under way, once every SM has its blocks
-  const int rounds = rounds_all * P.H >= 4ll * 8 * h->num_sms ? 8 : (rounds_all * P.H >= 4ll * 2 * h->num_sms ? 2 : 1);
+  const int rounds = rounds_all * P.H >= 4ll * most * h->num_sms ? most : (rounds_all * P.H >= 4ll * 2 * h->num_sms ? 2 : 1);
   const long long blocks = (rounds_all + rounds - 1) / rounds * P.H;
   if (blocks > 0x7fffffffll) return FC_ERR_UNSUPPORTED;
   cudaLaunchConfig_t lc = {};
@@ -402,8 +409,8 @@ extern "C" fc_status fc_quantize_cache(fc_handle *h, const fc_kv_view *kv, const
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if ((s = fc_flush_pending(h, st)) != FC_OK) return s;
   const bool wide = cache->head_dim == 128;
-  if (cache->dtype == FC_F16) return launch_rows(h, wide ? k_quantize<__half, 128> : k_quantize<__half, 64>, P, cache->head_dim, st);
-  return launch_rows(h, wide ? k_quantize<__nv_bfloat16, 128> : k_quantize<__nv_bfloat16, 64>, P, cache->head_dim, st);
+  if (cache->dtype == FC_F16) return launch_rows(h, wide ? k_quantize<__half, 128> : k_quantize<__half, 64>, P, cache->head_dim, 8, st);
+  return launch_rows(h, wide ? k_quantize<__nv_bfloat16, 128> : k_quantize<__nv_bfloat16, 64>, P, cache->head_dim, 8, st);
 }
 
 extern "C" fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k, void *out_v, int64_t rows,
@@ -423,6 +430,6 @@ extern "C" fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, v
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if ((s = fc_flush_pending(h, st)) != FC_OK) return s;
   const bool wide = cache->head_dim == 128;
-  if (cache->dtype == FC_F16) return launch_rows(h, wide ? k_dequantize<__half, 128> : k_dequantize<__half, 64>, P, cache->head_dim, st);
-  return launch_rows(h, wide ? k_dequantize<__nv_bfloat16, 128> : k_dequantize<__nv_bfloat16, 64>, P, cache->head_dim, st);
+  if (cache->dtype == FC_F16) return launch_rows(h, wide ? k_dequantize<__half, 128> : k_dequantize<__half, 64>, P, cache->head_dim, 2, st);
+  return launch_rows(h, wide ? k_dequantize<__nv_bfloat16, 128> : k_dequantize<__nv_bfloat16, 64>, P, cache->head_dim, 2, st);
 }
