@@ -4,7 +4,7 @@
 // rows, then the 16-bit tail.  A step reads every visible row once; the frame is that of fc_decode.cu: the tiles of all
 // sequences and heads form one line, one block per SM takes an equal share of it, a warp keeps a ring of tiles in flight, the
 // other warps only ever wait for the tile they use, blocks that share a sequence meet in a second kernel.
-// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 34 us, 3.2 TB/s; 41769 rows of 32 heads 49.5 us, 3.9 TB/s: some
+// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 33.8 us, 3.2 TB/s; 41770 rows of 32 heads 48.7 us, 4 TB/s: some
 // 7 us for two launches, the first tile and the joins, the rest bound by the instructions (0.53 a cycle and scheduler, over the
 // whole kernel; a 4-bit row has 3.6 times the arithmetic per byte of a 16-bit one).  A step over 820 rows takes 7.3 us.
 //
@@ -38,7 +38,7 @@ constexpr int kTeams = 3;                      // that take the tiles of a block
 constexpr int kWarps = kTeam * kTeams;         // consumer warps; the first of four more loads
 constexpr int kConsumers = 32 * kWarps;
 constexpr int kThreads = kConsumers + 128;
-// Registers of a thread: 128 at launch, moved from the loading warps to the others (with 152 instead of 160 a step over 41769
+// Registers of a thread: 128 at launch, moved from the loading warps to the others (with 152 instead of 160 a step over 41770
 // rows of 32 heads takes 52 us instead of 49).
 constexpr int kRegsLaunch = 128, kRegsLoad = 32, kRegsRows = 160;
 static_assert(kRegsLoad + kTeams * kRegsRows <= kRegsLaunch * (kTeams + 1), "a register split has to come out of what was launched");
