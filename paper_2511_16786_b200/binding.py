@@ -559,6 +559,8 @@ def fc_quantize_cache(handle, k, v, cache: Cache4, used=None, out_rows=None) -> 
         _counter(used, "used", 1)
     if out_rows is not None:
         _counter(out_rows, "out_rows", rows)
+    if rows == 0:
+        return
     view = fc_kv_view(k.data_ptr(), v.data_ptr(), strides[0], strides[1], _DTYPE[dtype], heads, d, 1, _two_ints(0, rows))
     rc = _lib.fc_quantize_cache(handle, byref(view), cache.ref, None if used is None else used.data_ptr(),
                                 None if out_rows is None else out_rows.data_ptr(), _stream_of(k))
@@ -576,6 +578,8 @@ def fc_dequantize_cache(handle, cache: Cache4, out_k, out_v, used=None) -> None:
     _same_device(out_k, out_v, cache.codes_k, used)
     if used is not None:
         _counter(used, "used", 1)
+    if rows == 0:
+        return
     rc = _lib.fc_dequantize_cache(handle, cache.ref, out_k.data_ptr(), out_v.data_ptr(), rows, None if used is None else used.data_ptr(),
                                   _stream_of(out_k))
     if rc != FC_OK:
@@ -655,6 +659,8 @@ def make_window_args(q, k, v, cu_seqlens_q, cu_seqlens_k, window: int, sinks: in
     # strides of single heads and tokens may be anything in a tensor
     view.stride_head = k.stride(1) if k.shape[1] > 1 else k.shape[2]
     view.stride_token = k.stride(0) if k.shape[0] > 1 else k.shape[1] * k.shape[2]
+    if k.shape[0] == 0:                  # without any key nothing is read, but empty tensors have no address
+        view.k = view.v = q.data_ptr()
     a = fc_window_args(q=q.data_ptr(), q_stride_token=q.stride(0) if q.shape[0] > 1 else q.shape[1] * q.shape[2],
                        q_stride_head=q.stride(1) if q.shape[1] > 1 else q.shape[2], num_q_heads=int(q.shape[1]), window=int(window),
                        sinks=int(sinks), cu_seqlens_q=ctypes.cast(cq, POINTER(c_int32)), kv=ctypes.pointer(view))
@@ -664,6 +670,8 @@ def make_window_args(q, k, v, cu_seqlens_q, cu_seqlens_k, window: int, sinks: in
 
 
 def fc_window_workspace_bytes(handle, args) -> int:
+    if args.q is None:                   # no queries
+        return 256
     n = int(_lib.fc_window_workspace_bytes(handle, byref(args)))
     if n == 0:
         raise FlashCacheError(1, "fc_window_workspace_bytes")
@@ -672,7 +680,10 @@ def fc_window_workspace_bytes(handle, args) -> int:
 
 def fc_window_attention(handle, args, out, workspace) -> None:
     """out: contiguous [Tq, Hq, d] of q's type."""
-    _check_out(args._device, out, workspace, args.cu_seqlens_q[args.kv.contents.batch])
+    tokens = args.cu_seqlens_q[args.kv.contents.batch]
+    _check_out(args._device, out, workspace, tokens)
+    if tokens == 0:
+        return
     rc = _lib.fc_window_attention(handle, byref(args), out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(args._device))
     if rc != FC_OK:
         raise FlashCacheError(rc, "fc_window_attention")
@@ -757,6 +768,8 @@ def make_rotary_args(positions, freq, q=None, out_q=None, k=None, out_k=None, v=
 
 
 def fc_rotary(handle, args) -> None:
+    if args.tokens == 0:                 # empty tensors have no address
+        return
     rc = _lib.fc_rotary(handle, byref(args), _stream_of(args._device))
     if rc != FC_OK:
         raise FlashCacheError(rc, "fc_rotary")

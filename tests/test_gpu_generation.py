@@ -236,3 +236,30 @@ def test_two_handles_on_two_streams_at_once(fc):
     for i in range(2):
         for a, b in got[i]:
             assert torch.equal(a, want[i][0]) and torch.equal(b, want[i][1])
+
+
+def test_nothing_to_do(fc):
+    """Empty tensors, which have no address, in every place that may be empty."""
+    handle = fc.fc_create(0, 1024)
+    empty = torch.empty((0, 4, 64), dtype=torch.float16, device="cuda")
+    some = torch.ones((5, 4, 64), dtype=torch.float16, device="cuda")
+    freq, _ = fc.fc_rotary_frequencies(64)
+    fc.fc_rotary(handle, fc.make_rotary_args(torch.empty(0, dtype=torch.int64, device="cuda"), freq, q=empty, out_q=empty, k=empty, out_k=empty))
+    cache = fc.Cache4.empty(16, 4, 64, torch.float16)
+    fc.fc_quantize_cache(handle, empty, empty, cache)
+    fc.fc_dequantize_cache(handle, cache, empty, empty)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    for q, k, cq, ck in ((empty, empty, [0, 0], [0, 0]), (empty, some, [0, 0], [0, 5]), (some, empty, [0, 2, 5], [0, 0, 0])):
+        args = fc.make_window_args(q, k, k, cq, ck, 3)
+        assert 0 < fc.fc_window_workspace_bytes(handle, args) <= ws.nbytes
+        out = torch.full_like(q, 7.0)
+        fc.fc_window_attention(handle, args, out, ws)
+        assert not out.any()                                       # queries that see nothing
+    offs = torch.zeros(6, dtype=torch.int64, device="cuda")
+    for held in (cache, (some, some)):
+        out = torch.full_like(some, 7.0)
+        dec = fc.make_decode_args_ex(some, held, offs, 0)
+        fc.fc_decode_attention_ex(handle, *dec, out, torch.empty(fc.fc_decode_workspace_bytes_ex(handle, *dec), dtype=torch.uint8, device="cuda"))
+        assert not out.any()
+    assert fc.fc_last_device_status(handle) == 0
+    fc.fc_destroy(handle)
