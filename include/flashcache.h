@@ -407,7 +407,8 @@ fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k,
  *   window    0: every row is visible.  Else, of a sequence's n rows (kept ones, then the tail), only the last `window`
  *   sinks     and the first `sinks` are; the others are not read (whole tiles of them).
  * Rows without weight (outside the window, or past a sequence's end) may hold anything.  A sequence without rows gives zeros
- * (a query whose scores are all minus infinity NaN: 0 / 0).
+ * (a query whose scores are all minus infinity NaN: 0 / 0).  bf16 values past 2^60 may overflow the fp32 sums that are
+ * divided at the end.
  */
 typedef struct {
   const fc_cache4 *cache4;
@@ -425,7 +426,8 @@ fc_status fc_decode_attention_ex(fc_handle *h, const fc_decode_args *a, const fc
  * window >= n_k: plain causal attention.  A query that sees no key (p < 0) gives zeros, one whose scores are all minus
  * infinity NaN (0 / 0).  fp32 scores, statistics and sums;
  * weights are rounded to dtype before the second product.  A key or value that is not finite reaches the queries that see
- * it and no other.
+ * it and no other.  Outputs are fp32 sums of values times weights of up to 2^24 (fp16: 2^14) before they are divided by the
+ * weights' sum, so bf16 values past 2^90 may overflow.
  *
  *   q            DEVICE [Tq][num_q_heads][head_dim] with strides (elements, channel stride 1, 16-byte aligned)
  *   kv           keys and values: FC_F16 or FC_BF16, head_dim 64 or 128; query head j reads KV head j / (num_q_heads / num_heads)

@@ -8,7 +8,7 @@
 // take turns, and the tensor cores have work for 2050 of some 3100 cycles.  32768 tokens of 28 heads over 4 (d = 128, bf16, window
 // 4096): 1.755 ms back to back, where the GPU runs at its power limit, 1.58 ms alone (1030 and 1145 TFLOP/s).
 //
-//  * Queries are taken in tiles of 128 rows, two to a block that share one stream of key tiles (128 keys).  A row is a query of one
+//  * Queries are taken in tiles of 128 rows, two to a block (one at d = 64) that share one stream of key tiles (128 keys).  A row is a query of one
 //    head; the query heads that share a KV head lie side by side in a tile (128 / G queries each), so keys are read once for
 //    all of them and a tile spans few positions: little of a short window is masked away.
 //  * Both products run on tcgen05: scores S = Q K^T from shared memory, outputs O += P V with the weights P (16 bits, written over
@@ -374,7 +374,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
 #pragma unroll
               for (int c = 4 * half; c < 4 * half + 4; ++c)
                 if ((steps >> c) & 1u) mma_ts(lead, tmem + 128u * (NT + q), tmem + 128u * q + 8u * c, vb + (unsigned)vs * (S::kTileBytes / 16) + 128u * c, hi, o_desc, 1u);
-              if (half == 0) umma::commit(lead, &sh.halved[q]);
+              if (D == 128 && half == 0) umma::commit(lead, &sh.halved[q]);          // for rows that go on with a reference that moved
             }
             if (!ok) break;
             ++turn[q];
