@@ -22,7 +22,8 @@
 //    d = 64 a ragged batch 41.3 us with an eighth, 42.4 with a quarter).
 //  * The reference m moves only when a score passes it by 14 (fp16) or 24 (bf16), so the outputs are rarely rescaled, and weights stay
 //    finite.  At d = 128 that none did is read off the sums of the weights; the largest score is only looked for where one did,
-//    in a row's first tile and in tiles seen in part (1807 -> 1773 us; at d = 64, where most tiles are such, 42 -> 46 us).
+//    in a row's first tile and in tiles seen in part (1807 -> 1773 us; the polynomial's upper end, which that needs, takes 11 of them
+//    back; at d = 64, where most tiles are such, 42 -> 46 us).
 //  * Values that are not finite: a product takes 0 x NaN from keys that a row does not see.  Tiles that some row sees in part
 //    are looked through by two more warps, which clear what is not finite and note the keys; rows that see such a key then
 //    add weight x value by themselves.  (Tiles seen by every row need nothing; nor do keys, whose scores are masked.)
@@ -156,12 +157,21 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // Two powers of two without the special-function units, which give 16 a cycle and SM and are what the weights wait for: the
 // nearest whole number into the exponent, the rest (at most half) by the polynomial of degree 4 with the smallest largest relative
 // error on [-1/2, 1/2] (2.7e-6, found by linear programming over 4001 points).  From -126 on down it stays at 2^-126, so it is
-// for tiles without masked scores; NaN becomes something above 2^127.
+// for tiles without masked scores; NaN becomes something above 2^127.  UP: from 127 on it stays at 2^127.  Without, x is below 128: the
+// exponent would run into the sign, and what comes out be small or negative.
+template <bool UP>
 __device__ __forceinline__ float2 exp2_poly(float2 x) {
   x = make_float2(max_nan(x.x, -126.f), max_nan(x.y, -126.f));
+  if (UP) x = make_float2(min_nan(x.x, 127.f), min_nan(x.y, 127.f));
   const float2 r = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));                     // 1.5 * 2^23: the last bits are the number
   const float2 n = __fadd2_rn(r, make_float2(-12582912.f, -12582912.f));
   const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
@@ -464,13 +474,14 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       tm_wait_ld(s);
       float2 sum;
       unsigned pk[32];
-      auto weights = [&](int c, float ref) {                       // of the keys c .. c + 63, all seen by all
+      // Weights of the keys c .. c + 63, all seen by all.  any: their scores may be any distance above the reference.
+      auto weights = [&](int c, float ref, auto any) {
         const float2 minus = make_float2(-ref, -ref);
         sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           const float2 x = __ffma2_rn(make_float2(s[c + 2 * j], s[c + 2 * j + 1]), scale, minus);
-          const float2 y = (j & (D == 128 ? 3 : 7)) == 3 ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          const float2 y = (j & (D == 128 ? 3 : 7)) == 3 ? exp2_poly<decltype(any)::value>(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
           sum = __fadd2_rn(sum, y);
           pk[j] = Mma<T>::pack(y.x, y.y);
         }
@@ -487,16 +498,16 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
         l += sum.x + sum.y;
       };
       // As a rule the reference stays as it is, and that it may shows in the sums: a weight that passes its bound makes a sum that does
-      // (so does NaN).  No largest score is looked for then.
+      // (so does NaN): none is negative, and one that no number holds is infinite or 2^127.  No largest score is looked for then.
       const bool quick = D == 128 && !looked && turn > 1u && !__any_sync(0xffffffffu, have && m == -INFINITY);
       bool begun = false;                                          // the first half is the product's already
       if (quick) {
         const float ref = m == -INFINITY ? 0.f : m;
         auto fits = [&]() { return !__any_sync(0xffffffffu, have && !(sum.x + sum.y <= kMost<T>)); };
-        weights(0, ref);
+        weights(0, ref, std::true_type());
         if (fits()) {
           give(0);
-          weights(64, ref);
+          weights(64, ref, std::true_type());
           if (fits()) {
             give(1);
             continue;
@@ -555,10 +566,10 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       const float ref = top != top ? top : (m == -INFINITY ? 0.f : m);                       // a NaN among the scores: all weights
       if (!looked) {                                               // the product starts on half of them
         if (!begun) {
-          weights(0, ref);
+          weights(0, ref, std::false_type());
           give(0);
         }
-        weights(64, ref);
+        weights(64, ref, std::false_type());
         give(1);
       } else {
         const float2 minus = make_float2(-ref, -ref);

@@ -171,6 +171,27 @@ def test_single_keys_far_above_the_rest(handle, at, much, d, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("times", [1, 2])
+def test_keys_whose_weight_passes_what_an_exponent_holds(handle, times, d, dtype):
+    """Keys so far above the rest that 2^(score - reference) has no number of 32 bits, in the second tile of a block, which all
+    queries see whole.  Each key-value head has other keys and another distance; with times = 2 there are blocks enough not
+    to split the keys.  Every second query head turns away from the key."""
+    places = [(128 + x,) for x in (6, 7, 62, 63, 70, 71, 126, 127)] + [(134, 135), (134, 190), (198, 255), (135, 199)]
+    heads = [(at, much) for at in places for much in (130.0, 200.0, 270.0, 400.0, 512.0)]
+    nq, nk, H, g = 70, 900, len(heads), torch.Generator().manual_seed(d)
+    base = torch.randn((H, 1, d), generator=g)
+    q = base * torch.tensor([1.0, -1.0])[:, None] + 0.1 * torch.randn((nq, H, 2, d), generator=g)
+    k, v = (0.3 * torch.randn((nk, H, d), generator=g) for _ in range(2))
+    for h, (at, much) in enumerate(heads):
+        for i, key in enumerate(at):
+            k[key, h] = base[h, 0] / (base[h, 0] @ base[h, 0]) * much * (1 + i / 4) * math.sqrt(d) * math.log(2.0)
+    q, k, v = (x.to(dtype).cuda() for x in (q.reshape(nq, 2 * H, d).repeat(1, times, 1), k.repeat(1, times, 1), v.repeat(1, times, 1)))
+    _check(_run(handle, q, k, v, [nq], [nk], 5000, 0), *_definition(q, k, v, [nq], [nk], 5000, 0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("nq,nk", [([700], [700]), ([4], [6000])])
 def test_scores_that_are_all_minus_infinity_are_undefined(handle, nq, nk, dtype):
     """0 / 0 by the definition, for the queries whose window holds such keys only; the others give them no weight."""
