@@ -403,7 +403,8 @@ fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k,
  *
  *   cache4    NULL: the kept rows are args' cache_k and cache_v.  Else they are held in 4 bits and args' cache_k, cache_v
  *             and cache_rows are not read; dtype, num_heads and head_dim are args'.  The tail is in 16 bits either way.
- *             Sums and softmax statistics in fp32; a weight is rounded to fp16 (11 bits) once, beside its row's scale.
+ *             Sums and softmax statistics in fp32; weight * scale is rounded to fp16 once, to 11 bits or to 2^-33 of the largest
+ *             such product of the query and half, whichever is coarser; weights below 2^-100 of a query's largest are none.
  *   window    0: every row is visible.  Else, of a sequence's n rows (kept ones, then the tail), only the last `window`
  *   sinks     and the first `sinks` are; the others are not read (whole tiles of them).
  * Rows without weight (outside the window, or past a sequence's end) may hold anything.  A sequence without rows gives zeros

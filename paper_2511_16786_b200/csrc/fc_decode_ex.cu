@@ -4,7 +4,7 @@
 // rows, then the 16-bit tail.  A step reads every visible row once; the frame is that of fc_decode.cu: the tiles of all
 // sequences and heads form one line, one block per SM takes an equal share of it, a warp keeps a ring of tiles in flight, the
 // other warps only ever wait for the tile they use, blocks that share a sequence meet in a second kernel.
-// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 33.8 us, 3.2 TB/s; 41770 rows of 32 heads 48.7 us, 4 TB/s: some
+// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 34.2 us, 3.2 TB/s; 41770 rows of 32 heads 50.0 us, 3.9 TB/s: some
 // 7 us for two launches, the first tile and the joins, the rest bound by the instructions (0.53 a cycle and scheduler, over the
 // whole kernel; a 4-bit row has 3.6 times the arithmetic per byte of a 16-bit one).  A step over 820 rows takes 7.3 us.
 //
@@ -18,8 +18,11 @@
 //    of a query stays with it, and eight columns are enough for 8 query heads (queries as rows: 43 and 61 us).
 //  * Four warps share a tile of 128 rows, 32 each, and three such teams take the tiles by turns (two: 43 and 66 us, queries as rows).
 //  * Queries are brought to 2^14 .. 2^15 by a power of two before they become half numbers (exact but for channels 2^-25 of the
-//    largest); weights are kept below 2^15 together with the largest scale met so far, so rounding them to half numbers (11 bits)
-//    neither overflows nor loses the small ones, whatever the range of the cache's type.
+//    largest).  Weight * scale becomes one at a power of two of its own, which a query has for either half of its output and which
+//    follows the largest such product, not the largest weight or the largest scale: the rounding (11 bits, or 2^-33 of that product)
+//    neither overflows nor loses rows beside one whose scale is large and whose weight is not, whatever the range of the cache's
+//    type.  (With one power for all, of the largest scale met: 48.7 instead of 50.0 us over the 41770 rows, 33.4 instead of 36.5
+//    over 100000 rows of 4 heads with 12 query heads each, but a row lost bits from 2^25 times its scale on.)
 //  * Kept rows of 16 bits and tails come in tiles of 32 rows (two warps each, 16 KB at d = 128, about what 128 rows of 4 bits take),
 //    so every tile of the line costs about the same.
 //  * A window makes of a sequence's tiles the first few and the last ones; rows of them that are not visible get no weight.
@@ -45,7 +48,14 @@ static_assert(kRegsLoad + kTeams * kRegsRows <= kRegsLaunch * (kTeams + 1), "a r
 constexpr int kRows4 = 32 * kTeam;             // rows of a 4-bit tile
 constexpr int kRows16 = 32;                    // rows of a 16-bit tile
 constexpr int kMaxBlocks = 256;                // blocks of a launch, at most
-constexpr float kTop = 14.f, kReset = 10.f;    // weights times the largest scale: at most 2^kTop, 2^kReset after a move
+// Weights are 2^(score - reference).  A reference moves up, so that the largest weight is 2^kReset, where one passes 2^kTop: in 16 bits
+// none overflows then, and weights down to 2^-24 of the largest keep all bits.
+constexpr float kTop = 14.f, kReset = 10.f;
+// Beside 4-bit tiles weights stay in fp32 and are 2^kDown smaller, so that sums of weight * minimum do not overflow, whatever the
+// values are.  There weight * scale is kept to these bounds, by a power of two of its own, kMostUp at most.
+constexpr float kDown = 34.f, kMostUp = 126.f;
+constexpr float kDownPower = 0x1p34f, kMostUpPower = 0x1p126f;
+constexpr float kNothing = -3e38f;             // reference of a query that has seen nothing yet
 
 struct ExParams {
   const void *q;
@@ -382,73 +392,105 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
       for (int r = 0; r < NQ; ++r) oacc[i][r][0] = oacc[i][r][1] = oacc[i][r][2] = oacc[i][r][3] = 0.f;
     float2 omin[NQ][2] = {};                   // sums of weight * minimum over this lane's rows, for its two queries (+8)
     float2 m[NQ], l[NQ] = {};                  // reference of the weights (log2), and their sum over this lane's rows
+    float2 up[NQ][2];                          // the power of two that the output of either half is held times, beside 4-bit tiles
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) m[r] = make_float2(-INFINITY, -INFINITY);
-    float vtop = 0.f, vexp = 0.f;              // a power of two that no value scale met so far passes, and its exponent (0: none yet)
+    for (int r = 0; r < NQ; ++r) {
+      m[r] = make_float2(kNothing, kNothing);
+      up[r][0] = up[r][1] = make_float2(kMostUpPower, kMostUpPower);
+    }
     bool in4 = false, have_q = false;
-    auto to_one = [&]() {                      // output from the units of 4-bit tiles to 1
+    auto to_one = [&](float more) {            // from the units of 4-bit tiles to 1; more: of what the weights are taken times
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int r = 0; r < NQ; ++r) {
+        l[r].x *= more; l[r].y *= more;
 #pragma unroll
-        for (int r = 0; r < NQ; ++r) {
-          oacc[i][r][0] *= 16777216.f; oacc[i][r][1] *= 16777216.f;
-          oacc[i][r][2] *= 1048576.f; oacc[i][r][3] *= 1048576.f;
+        for (int u = 0; u < 2; ++u) {
+          omin[r][u].x *= more; omin[r][u].y *= more;
+          const float d0 = __uint_as_float(0x7f000000u - __float_as_uint(up[r][u].x)) * more;      // more / up
+          const float d1 = __uint_as_float(0x7f000000u - __float_as_uint(up[r][u].y)) * more;
+#pragma unroll
+          for (int i = u * (MT / 2); i < (u + 1) * (MT / 2); ++i) {
+            oacc[i][r][0] = oacc[i][r][0] * 16777216.f * d0; oacc[i][r][1] = oacc[i][r][1] * 16777216.f * d1;
+            oacc[i][r][2] = oacc[i][r][2] * 1048576.f * d0; oacc[i][r][3] = oacc[i][r][3] * 1048576.f * d1;
+          }
         }
+      }
     };
     auto over_rows = [&](float x) {            // the lanes that have the same columns
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
       return x;
     };
-    // New scores, the lane's largest of either column: the references move where any lane needs it.
-    auto refer = [&](float2 (&x)[NQ], float es) {
-      bool move = es > vtop;
+    // Scores beside 16-bit rows, the lane's largest of either column: the references move where any lane needs it.
+    auto refer = [&](const float2 (&x)[NQ]) {
+      bool move = false;
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) move |= x[r].x + vexp > m[r].x + kTop || x[r].y + vexp > m[r].y + kTop;
+      for (int r = 0; r < NQ; ++r) move |= x[r].x > m[r].x + kTop || x[r].y > m[r].y + kTop;
       if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) es = fmaxf(es, __shfl_xor_sync(0xffffffffu, es, o));
-        if (es > vtop) {                       // a larger scale than any before
-          int e = (int)(__float_as_uint(es) >> 23) + 1;                    // es < 2^(e - 127)
-          e = e < 87 ? 87 : (e > 254 ? 254 : e);                           // not below 2^-40: sums of weights stay finite
-          vtop = __uint_as_float((unsigned)e << 23);
-          vexp = (float)(e - 127);
-        }
-#pragma unroll
         for (int r = 0; r < NQ; ++r) {
-          const float n0 = over_rows(x[r].x) + vexp, n1 = over_rows(x[r].y) + vexp;
+          const float n0 = over_rows(x[r].x), n1 = over_rows(x[r].y);
           const float t0 = n0 > m[r].x + kTop ? n0 - kReset : m[r].x, t1 = n1 > m[r].y + kTop ? n1 - kReset : m[r].y;
-          // by half the exponent, twice: scales may grow by 2^165, and weights of 2^50 then become such of 2^-115
-          const float c0 = m[r].x == t0 ? 1.f : exp2f(0.5f * (m[r].x - t0)), c1 = m[r].y == t1 ? 1.f : exp2f(0.5f * (m[r].y - t1));
+          const float c0 = exp2f(m[r].x - t0), c1 = exp2f(m[r].y - t1);
           m[r] = make_float2(t0, t1);
+          l[r].x *= c0; l[r].y *= c1;
+          omin[r][0].x *= c0; omin[r][0].y *= c1;
+          omin[r][1].x *= c0; omin[r][1].y *= c1;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            l[r].x *= c0; l[r].y *= c1;
-            omin[r][0].x *= c0; omin[r][0].y *= c1;
-            omin[r][1].x *= c0; omin[r][1].y *= c1;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-              oacc[i][r][0] *= c0; oacc[i][r][1] *= c1;
-              oacc[i][r][2] *= c0; oacc[i][r][3] *= c1;
-            }
+          for (int i = 0; i < MT; ++i) {
+            oacc[i][r][0] *= c0; oacc[i][r][1] *= c1;
+            oacc[i][r][2] *= c0; oacc[i][r][3] *= c1;
           }
         }
       }
     };
-    // what is subtracted from scores (a query that has seen nothing yet only has scores of minus infinity)
-    auto minus = [&](const float2 &x) { return make_float2(x.x == -INFINITY ? 0.f : -x.x, x.y == -INFINITY ? 0.f : -x.y); };
+    // The same beside 4-bit rows, 8 N of them: a query's reference follows its largest score, and the power of two of a half of its output
+    // the largest weight * scale of that half, each for itself: a row with a large scale but no weight holds nothing down, nor does
+    // the other half.  Whole steps only, so that the powers stay exact.
+    constexpr int JJ = NQ == 1 ? 2 : 1, N = 2 * JJ;
+    auto refer4 = [&](int r, const float2 (&x)[N], const unsigned (&vp)[N][2]) {
+      float2 n = x[0];
+#pragma unroll
+      for (int b8 = 1; b8 < N; ++b8) n = make_float2(fmaxf(n.x, x[b8].x), fmaxf(n.y, x[b8].y));
+      auto moved = [&](float top, float was) { return top > was + (kTop - kDown) ? ceilf(top) - (kReset - kDown) : was; };
+      const float2 to = make_float2(moved(over_rows(n.x), m[r].x), moved(over_rows(n.y), m[r].y));
+      const float2 by = make_float2(to.x - m[r].x, to.y - m[r].y), c = make_float2(exp2f(-by.x), exp2f(-by.y));
+      m[r] = to;
+      l[r].x *= c.x; l[r].y *= c.y;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        omin[r][u].x *= c.x; omin[r][u].y *= c.y;
+        float2 z = make_float2(-INFINITY, -INFINITY);                    // weight * scale < 2^z
+#pragma unroll
+        for (int b8 = 0; b8 < N; ++b8) {
+          const float e = (float)((int)((__float_as_uint(two<T>(vp[b8][u]).x) >> 23) & 255u) - 126);
+          z = make_float2(fmaxf(z.x, x[b8].x - to.x + e), fmaxf(z.y, x[b8].y - to.y + e));
+        }
+        // `was`: the exponent of `up` if the output so far stayed as it is
+        auto held = [&](float most, float was) { was = fminf(was, kMostUp); return most + was > kTop ? floorf(kReset - most) : was; };
+        auto exponent = [](float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); };
+        auto power = [](float e) { return __uint_as_float((unsigned)((int)e + 127) << 23); };
+        const float2 was = make_float2(exponent(up[r][u].x) + by.x, exponent(up[r][u].y) + by.y);
+        const float2 e = make_float2(held(over_rows(z.x), was.x), held(over_rows(z.y), was.y));
+        const float2 f = make_float2(exp2f(e.x - was.x), exp2f(e.y - was.y));
+        up[r][u] = make_float2(power(e.x), power(e.y));
+#pragma unroll
+        for (int i = u * (MT / 2); i < (u + 1) * (MT / 2); ++i) {
+          oacc[i][r][0] *= f.x; oacc[i][r][1] *= f.y;
+          oacc[i][r][2] *= f.x; oacc[i][r][3] *= f.y;
+        }
+      }
+    };
     // 16 JJ rows of a 4-bit tile at shared address `tile_p`, from its row `first` on.
     // (With 16 query heads the registers are enough for 16 rows at a time.)
-    constexpr int JJ = NQ == 1 ? 2 : 1;
     // `visible`: a bit for each of them.
     auto rows4 = [&](unsigned tile_p, int first, unsigned visible) {
       // operand row g of 8 is row `mine` of the tile's 8, so that the values' lanes (rows t and 7 - t) meet fewer bank conflicts
       const int mine = (g & 1) ? 7 - (g >> 1) : (g >> 1);
       const unsigned kc = tile_p + (unsigned)((first + mine) * S::kCode + t * (D / 8));
       const unsigned kpar = tile_p + (unsigned)(2 * kRows4 * S::kCode + (first + mine) * S::kParam);
-      float2 sc[NQ][2 * JJ], top[NQ];                                           // [8 rows]: the lane's row, its two queries
-      unsigned vp[2 * JJ][2];                                                   // (scale, minimum) of its values, [half]
-      float es = 0.f;
+      float2 sc[NQ][N];                                                         // [8 rows]: the lane's row, its two queries
+      unsigned vp[N][2];                                                        // (scale, minimum) of its values, [half]
 #pragma unroll
       for (int jj = 0; jj < JJ; ++jj) {                                     // 16 rows: operand rows g and g + 8
         unsigned w[2][D / 32];
@@ -503,32 +545,45 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
             for (int r = 0; r < NQ; ++r) sc[r][b8] = make_float2(-INFINITY, -INFINITY);
           }
       }
-#pragma unroll
-      for (int b8 = 0; b8 < 2 * JJ; ++b8) es = fmaxf(es, fmaxf(two<T>(vp[b8][0]).x, two<T>(vp[b8][1]).x));
-#pragma unroll
-      for (int r = 0; r < NQ; ++r) {
-        top[r] = sc[r][0];
-#pragma unroll
-        for (int b8 = 1; b8 < 2 * JJ; ++b8) top[r] = make_float2(fmaxf(top[r].x, sc[r][b8].x), fmaxf(top[r].y, sc[r][b8].y));
-      }
-      refer(top, es);
-      unsigned pw[NQ][2][2 * JJ];                                               // [half][8 rows]: weight * scale as the right operand
+      // Weights by the references as they are.  That none passes its bound shows in their sums and products; only where one does is the
+      // largest looked for.
+      unsigned pw[NQ][2][N];                                                    // [half][8 rows]: weight * scale as the right operand
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
-        const float2 ref = minus(m[r]);
+        float2 sum, with_min[2];
+        auto weigh = [&]() {                                               // -> did a sum or a product pass
+          sum = make_float2(0.f, 0.f);
+          with_min[0] = omin[r][0];
+          with_min[1] = omin[r][1];
+          unsigned most = 0u;                                              // largest products of both queries, by their bits (a NaN's are larger)
 #pragma unroll
-        for (int b8 = 0; b8 < 2 * JJ; ++b8) {
-          const float2 x = __fadd2_rn(sc[r][b8], ref);
-          const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-          l[r] = __fadd2_rn(l[r], p);
+          for (int b8 = 0; b8 < N; ++b8) {
+            const float2 x = __fadd2_rn(sc[r][b8], make_float2(-m[r].x, -m[r].y));
+            const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+            sum = __fadd2_rn(sum, p);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float2 v = two<T>(vp[b8][u]);
-            pw[r][u][b8] = transposed(Mma<__half>::pack(p.x * v.x, p.y * v.x));
-            omin[r][u].x = fmaf(p.x, v.y, omin[r][u].x);
-            omin[r][u].y = fmaf(p.y, v.y, omin[r][u].y);
+            for (int u = 0; u < 2; ++u) {
+              const float2 v = two<T>(vp[b8][u]), w = __fmul2_rn(p, up[r][u]);
+              pw[r][u][b8] = Mma<__half>::pack(w.x * v.x, w.y * v.x);
+              with_min[u].x = fmaf(p.x, v.y, with_min[u].x);
+              with_min[u].y = fmaf(p.y, v.y, with_min[u].y);
+            }
+            most = __vimax3_u16x2(most, pw[r][0][b8], pw[r][1][b8]);
           }
+          // 2^14 as a half number; eight weights that no reference has to move for sum to no more than 2^-17
+          return !(sum.x + sum.y <= 0x1p-16f) || (most & 0xffffu) > 0x7400u || (most >> 16) > 0x7400u;
+        };
+        if (__any_sync(0xffffffffu, weigh())) {
+          refer4(r, sc[r], vp);
+          weigh();
         }
+        l[r] = __fadd2_rn(l[r], sum);
+        omin[r][0] = with_min[0];
+        omin[r][1] = with_min[1];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int b8 = 0; b8 < N; ++b8) pw[r][u][b8] = transposed(pw[r][u][b8]);
       }
       // values: run g of the rows t and 7 - t of every 8; nibble n of a run is channel 8 n + g
       const unsigned va = tile_p + (unsigned)((kRows4 + first) * S::kCode + g * (D / 16));
@@ -596,15 +651,14 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
           sc[r][j] = vis ? make_float2(acc[r][2 * j] * P.scale_log2, acc[r][2 * j + 1] * P.scale_log2) : make_float2(-INFINITY, -INFINITY);
       }
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) top[r] = make_float2(fmaxf(sc[r][0].x, sc[r][1].x) - vexp, fmaxf(sc[r][0].y, sc[r][1].y) - vexp);
-      refer(top, 0.f);                                                     // no scale beside these weights
+      for (int r = 0; r < NQ; ++r) top[r] = make_float2(fmaxf(sc[r][0].x, sc[r][1].x), fmaxf(sc[r][0].y, sc[r][1].y));
+      refer(top);
       unsigned pw[NQ][2];
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
-        const float2 ref = minus(m[r]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float2 x = __fadd2_rn(sc[r][j], ref);
+          const float2 x = __fadd2_rn(sc[r][j], make_float2(-m[r].x, -m[r].y));
           const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
           l[r] = __fadd2_rn(l[r], p);
           pw[r][j] = transposed(Mma<T>::pack(p.x, p.y));
@@ -653,7 +707,9 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
         if ((((warp % kTeam) >> 1) == (((n + i) / kTeams) & 1)) && row0 < end && (row0 < s.low || row0 + 15 >= s.high)) {
           if (!have_q) {                                                   // kept rows come before the tail: never back
             load_q16();
-            to_one();
+            to_one(kDownPower);
+#pragma unroll
+            for (int r = 0; r < NQ; ++r) m[r] = make_float2(m[r].x - kDown, m[r].y - kDown);
             have_q = true;
             in4 = false;
           }
@@ -665,11 +721,11 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     }
     n += cnt;
     ti = seg_end;
-    if (in4) to_one();
+    if (in4) to_one(1.f);
     if (failed) {
 #pragma unroll
       for (int r = 0; r < NQ; ++r) {
-        m[r] = make_float2(-INFINITY, -INFINITY);
+        m[r] = make_float2(kNothing, kNothing);
         l[r] = omin[r][0] = omin[r][1] = make_float2(0.f, 0.f);
       }
 #pragma unroll
@@ -719,19 +775,18 @@ k_decode_ex(const __grid_constant__ ExParams P, const __grid_constant__ ExMaps M
     const size_t slot = ((size_t)blk + (size_t)h * P.B + b) * P.G;
     constexpr int C = D / 32;                                              // channels per lane
     for (int r = warp; r < P.G; r += kWarps) {                             // a warp per query head
-      float mm = -INFINITY, ll = 0.f, o[C];
+      float mm = kNothing, ll = 0.f, o[C];
       for (int k = 0, w = warp0; k < parts; ++k, w = w + 1 == kWarps ? 0 : w + 1) mm = fmaxf(mm, mml[w * kHeads + r].x);
-      const float ref = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
       for (int c = 0; c < C; ++c) o[c] = 0.f;
 #pragma unroll 4
       for (int k = 0, w = warp0; k < parts; ++k, w = w + 1 == kWarps ? 0 : w + 1) {
         const float2 ml = mml[w * kHeads + r], mn = mmin[w * kHeads + r];
-        const float f = exp2f(0.5f * (ml.x - ref)), add = lane < 16 ? mn.x : mn.y;   // twice, as in `refer`
+        const float f = exp2f(ml.x - mm), add = lane < 16 ? mn.x : mn.y;
         const float *src = mo + ((size_t)w * kHeads + r) * S::kStride + C * lane;
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = fmaf((src[c] + add) * f, f, o[c]);
-        ll = fmaf(ml.y * f, f, ll);
+        for (int c = 0; c < C; ++c) o[c] = fmaf(src[c] + add, f, o[c]);
+        ll = fmaf(ml.y, f, ll);
       }
       if (i0 == i1) {
         const float inv = 1.f / ll;                                        // 0 only of scores that are all minus infinity: 0 / 0
@@ -776,20 +831,19 @@ k_decode_ex_combine(const __grid_constant__ ExParams P, int width) {
   float2 ml[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e)
-    ml[e] = tid + kThreadsC * e < cnt ? __ldcg(P.part_ml + slot0 + (unsigned)(tid + kThreadsC * e) * (unsigned)P.G) : make_float2(-INFINITY, 0.f);
+    ml[e] = tid + kThreadsC * e < cnt ? __ldcg(P.part_ml + slot0 + (unsigned)(tid + kThreadsC * e) * (unsigned)P.G) : make_float2(kNothing, 0.f);
   float m = fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (lane == 0) top[warp] = m;
   __syncthreads();
   m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-  const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const float f = exp2_fast(0.5f * (ml[e].x - ref));                     // the root of a result's weight (see `refer`)
+    const float f = exp2_fast(ml[e].x - m);
     weight[tid + kThreadsC * e] = f;
-    l = fmaf(f * ml[e].y, f, l);
+    l = fmaf(f, ml[e].y, l);
   }
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -800,7 +854,7 @@ k_decode_ex_combine(const __grid_constant__ ExParams P, int width) {
   for (int i = first;;) {
 #pragma unroll
     for (int a = 0; a < kAhead; ++a)
-      if (i + groups * a < cnt) acc = fmaf(v[a] * weight[i + groups * a], weight[i + groups * a], acc);
+      if (i + groups * a < cnt) acc = fmaf(v[a], weight[i + groups * a], acc);
     i += groups * kAhead;
     if (i >= cnt) break;
 #pragma unroll

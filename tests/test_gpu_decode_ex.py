@@ -220,6 +220,52 @@ def test_scales_at_both_ends_of_bf16(handle, most, apart):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 12])
+@pytest.mark.parametrize("large,far,tails", [(2.0 ** 30, 80.0, None), (2.0 ** 60, 80.0, None), (2.0 ** 60, 80.0, [70]), (2.0 ** 100, 110.0, None),
+                                             (2.0 ** 40, 0.0, None)])
+def test_rows_of_unlike_scales_hold_nothing_down(handle, large, far, tails, G, d):
+    """Some rows' values are `large` times the others', and their weights 2^-far times those, before, between and after the others
+    in every warp's rows; the odd query heads see it the other way round.  Values that small beside the large ones count."""
+    n, H, g = 128 * 9 + 77, 2, torch.Generator().manual_seed(int(far) + d)
+    rare = (torch.arange(n) // 8 % 3 == 0)
+    base = torch.randn((H, 1, d), generator=g)
+    q = (base * torch.tensor([1.0, -1.0]).repeat(G // 2)[:, None] + 0.05 * torch.randn((H, G, d), generator=g)).reshape(1, H * G, d)
+    k, v = 0.2 * torch.randn((n, H, d), generator=g), torch.randn((n, H, d), generator=g)
+    k[rare] -= (base / (base * base).sum(-1, keepdim=True) * far * math.sqrt(d) * math.log(2.0))[:, 0]
+    v[rare] *= large
+    q, k, v = (x.to(torch.bfloat16).cuda() for x in (q, k, v))
+    tail = [torch.randn((1, 80, H, d), generator=g).to(torch.bfloat16).cuda() for _ in range(2)] if tails else None
+    cache = fc.Cache4.empty(n, H, d, torch.bfloat16)
+    fc.fc_quantize_cache(handle, k, v, cache)
+    main = _held(cache.codes_k, cache.params_k, False) + _held(cache.codes_v, cache.params_v, True)
+    want, tol = _definition(q, main, [0, n], tail, tails, 0, 0, torch.bfloat16, True)
+    for most in (1, n):                                                    # few blocks, and many
+        _check(_run(handle, q, cache, [0, n], tail, tails, 0, 0, most=most), want, tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size,other", [(2.0 ** 40, 1.0), (2.0 ** -100, 1.0), (2.0 ** -100, 2.0 ** -100), (2.0 ** 120, 2.0 ** -90)])
+def test_halves_of_unlike_scales(handle, size, other, d):
+    """The halves of a row are held with scales of their own, and neither costs the other bits."""
+    lens, H, G = [700, 129], 2, 7
+    g = torch.Generator().manual_seed(17)
+    n = sum(lens)
+    q, k = (torch.randn(s, generator=g).to(torch.bfloat16).cuda() for s in ((2, H * G, d), (n, H, d)))
+    v = torch.randn((n, H, d), generator=g) + 0.5
+    v[:, 0, :d // 2] *= size
+    v[:, 1, d // 2:] *= size
+    v[:, 0, d // 2:] *= other
+    v[:, 1, :d // 2] *= other
+    cache = fc.Cache4.empty(n, H, d, torch.bfloat16)
+    fc.fc_quantize_cache(handle, k, v.to(torch.bfloat16).cuda(), cache)
+    main = _held(cache.codes_k, cache.params_k, False) + _held(cache.codes_v, cache.params_v, True)
+    want, tol = _definition(q, main, [0, 700, n], None, None, 0, 0, torch.bfloat16, True)
+    _check(_run(handle, q, cache, [0, 700, n], None, None, 0, 0), want, tol)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_scores_that_are_all_minus_infinity_are_undefined(handle, dtype):
     """0 / 0 by the definition, for the queries and sequences that see nothing else."""
