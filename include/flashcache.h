@@ -426,9 +426,9 @@ fc_status fc_decode_attention_ex(fc_handle *h, const fc_decode_args *a, const fc
  *     out[i] = Softmax over visible j (q[i] k[j] / sqrt(head_dim)) v[j],   j visible:  j <= p and (j > p - window or j < sinks).
  * window >= n_k: plain causal attention.  A query that sees no key (p < 0) gives zeros, one whose scores are all minus
  * infinity NaN (0 / 0).  fp32 scores, statistics and sums;
- * weights are rounded to dtype before the second product.  A key or value that is not finite reaches the queries that see
- * it and no other.  Outputs are fp32 sums of values times weights of up to 2^24 (fp16: 2^14) before they are divided by the
- * weights' sum, so bf16 values past 2^90 may overflow.
+ * weights are rounded to dtype before the second product (fp16: to 11 bits or to 2^-32 of the query's largest, whichever is
+ * coarser).  A key or value that is not finite reaches the queries that see it and no other.  Outputs are fp32 sums of values
+ * times weights of up to 2^24 (fp16: 2^16) before they are divided by the weights' sum, so bf16 values past 2^90 may overflow.
  *
  *   q            DEVICE [Tq][num_q_heads][head_dim] with strides (elements, channel stride 1, 16-byte aligned)
  *   kv           keys and values: FC_F16 or FC_BF16, head_dim 64 or 128; query head j reads KV head j / (num_q_heads / num_heads)

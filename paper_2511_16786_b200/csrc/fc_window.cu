@@ -20,7 +20,7 @@
 //  * A quarter of the exponentials (an eighth at d = 64) are polynomials: the special-function units give 16 a cycle and SM, so a
 //    128 x 128 tile would take 1024 cycles, as long as its two products at d = 128 (1770 us; an eighth 1797, three eighths 1807; at
 //    d = 64 a ragged batch 41.3 us with an eighth, 42.4 with a quarter).
-//  * The reference m moves only when a score passes it by 14 (fp16) or 24 (bf16), so the outputs are rarely rescaled, and weights stay
+//  * The reference m moves only when a score passes it by 15 (fp16) or 24 (bf16), so the outputs are rarely rescaled, and weights stay
 //    finite.  At d = 128 that none did is read off the sums of the weights; the largest score is only looked for where one did,
 //    in a row's first tile and in tiles seen in part (1807 -> 1773 us; the polynomial's upper end, which that needs, takes 11 of them
 //    back; at d = 64, where most tiles are such, 42 -> 46 us).
@@ -45,10 +45,15 @@ constexpr int kTileRows = 128;                 // query rows, and keys, of a til
 constexpr int kSeqs = 64;                      // sequences described per launch (kernel-argument table)
 constexpr int kValues = 4;                     // value tiles in the ring, at most
 constexpr int kSplitMin = 4;                   // key tiles that a part of a split has at least
-// How far, in powers of two, a score may pass its row's reference before that moves (and the outputs are rescaled): weights stay
-// below 2^14 in fp16, 2^24 in bf16, and one below 2^-24 of the reference's is nothing in either.
-template <typename T> constexpr float kSlack = std::is_same<T, __half>::value ? 14.f : 24.f;
-template <typename T> constexpr float kMost = std::is_same<T, __half>::value ? 0x1p14f : 0x1p24f;
+// How far, in powers of two, a score may pass its row's reference before that moves (and the outputs are rescaled), and how far it
+// is above it then: a row's largest weight is 2^7..2^15 in fp16, 1..2^24 in bf16.  A half number below 2^-14 has fewer bits and one of
+// 2^-25 is none, so a row loses 2^-32 of its largest weight at most for every key; with the largest at 1, 2^17 keys of 2^-25.5 each
+// would be missing in the output but not in the sum.  (16384 tokens of 28 heads, fp16, d = 128, window 4096: 738 us with 1 and with
+// 2^7, 747 with 2^8; with queries four times as long, whose references move more often, 900, 937 and 960.)  bf16 has fp32's exponents.
+template <typename T> constexpr float kSlack = std::is_same<T, __half>::value ? 15.f : 24.f;
+template <typename T> constexpr float kAbove = std::is_same<T, __half>::value ? 7.f : 0.f;
+// What a sum may come to that shows none of its weights to have passed what the type holds.
+template <typename T> constexpr float kMost = std::is_same<T, __half>::value ? 65504.f : 0x1p24f;
 
 struct WinSeq { int q0, nq, k0, nk, item; };   // item: first of the sequence's, in blocks before splitting
 
@@ -548,7 +553,7 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
       top *= P.scale_log2;
       const bool move = top > m + (quick ? kSlack<T> - 7.f : kSlack<T>);          // a sum of 64 has passed it
       if (__any_sync(0xffffffffu, move)) {
-        const float to = move ? top : m, f = m == to ? 1.f : exp2f(m - to);
+        const float to = move ? top - kAbove<T> : m, f = m == to ? 1.f : exp2f(m - to);
         m = to;
         l *= f;
         if (turn > 1u) {                                           // the products so far are done: the scores came after them

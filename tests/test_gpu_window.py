@@ -191,6 +191,28 @@ def test_keys_whose_weight_passes_what_an_exponent_holds(handle, times, d, dtype
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,nk", [(1, 20000), (80, 4000)])
+@pytest.mark.parametrize("key", [0, 1])
+@pytest.mark.parametrize("far", [16.0, 25.5, 28.0])
+def test_many_keys_far_below_one_are_not_lost_in_half_numbers(handle, far, key, H, nk, d):
+    """Thousands of keys whose weights are 2^-far of a first (or last) key's, which has a value of zero: the output is theirs.  A
+    weight is a half number in units of 2^-7 of a row's largest at most, so the rounding is off by half a step of the small ones,
+    2^-25 of those units: 2^-32 of the largest weight for every key, beside what holds for larger ones."""
+    nq, g = 40, torch.Generator().manual_seed(int(far) + d)
+    base = torch.randn(d, generator=g)
+    q = (base + 0.02 * torch.randn((nq, H, d), generator=g)).half().cuda()
+    k, v = 0.02 * torch.randn((nk, H, d), generator=g), 8 + 0.5 * torch.randn((nk, H, d), generator=g)
+    at = 0 if key == 0 else nk - nq
+    k[at] += base / (base @ base) * far * math.sqrt(d) * math.log(2.0)
+    v[at] = 0.0
+    k, v = k.half().cuda(), v.half().cuda()
+    want, tol = _definition(q, k, v, [nq], [nk], nk, 0)
+    tol += 2.0 ** -32 * v.double().abs().sum(0)                 # the largest weight is at most 1 of their sum
+    _check(_run(handle, q, k, v, [nq], [nk], nk, 0), want, tol)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("nq,nk", [([700], [700]), ([4], [6000])])
 def test_scores_that_are_all_minus_infinity_are_undefined(handle, nq, nk, dtype):
