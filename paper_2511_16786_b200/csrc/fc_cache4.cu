@@ -317,10 +317,10 @@ k_dequantize(const CacheParams P, int rounds) {
   constexpr int LANES = D / 16, ROWS = kQThreads / LANES;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  long long n = P.rows;
-  if (P.used) { const long long m = *P.used; n = m < n ? m : n; }
+  int rows = (int)P.rows;                            // fewer than 2^31
+  if (P.used) { const long long m = *P.used; rows = m < rows ? (int)(m < 0 ? 0 : m) : rows; }
   const unsigned h = blockIdx.x % (unsigned)P.H;
-  const int u = threadIdx.x % LANES, rows = (int)n;
+  const int u = threadIdx.x % LANES;
   int t = (int)(blockIdx.x / (unsigned)P.H) * rounds * ROWS + threadIdx.x / LANES;
   const int warp_row = t - (threadIdx.x & 31) / LANES;
   const size_t head = (size_t)h * P.cap;

@@ -231,3 +231,25 @@ def test_cache_argument_checks_of_the_binding(fc):
         fc.fc_dequantize_cache(h, c, k, k.half())
     with pytest.raises(fc.FlashCacheError):
         fc.fc_quantize_cache(h, k.half(), k.half(), c)
+
+
+@pytest.mark.parametrize("used", [0, -1, 5 - 2 ** 32, 5 - 2 ** 63, 2 ** 32 + 5])
+def test_counts_of_rows_outside_the_rows(fc, handle, used):
+    """Negative ones name no row, ones past the rows all of them, however many bits they have."""
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn((10, 3, 64), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    cache = fc.Cache4.empty(10, 3, 64, torch.bfloat16)
+    whole = [torch.empty_like(k), torch.empty_like(v)]
+    fc.fc_quantize_cache(handle, k, v, cache)
+    fc.fc_dequantize_cache(handle, cache, *whole)
+    count = torch.tensor([used], device="cuda")
+    outs = [torch.full_like(k, 7.0), torch.full_like(v, 7.0)]
+    fc.fc_dequantize_cache(handle, cache, *outs, used=count)
+    other = fc.Cache4.empty(10, 3, 64, torch.bfloat16)
+    for t in (other.codes_k, other.codes_v, other.params_k, other.params_v):
+        t.fill_(7)
+    before = other.codes_k.clone()
+    fc.fc_quantize_cache(handle, k, v, other, used=count)
+    for out, all_of_them in zip(outs, whole):
+        assert torch.equal(out, all_of_them if used > 0 else torch.full_like(out, 7.0))
+    assert torch.equal(other.codes_k[:, :10], cache.codes_k[:, :10] if used > 0 else before[:, :10])
