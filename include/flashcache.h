@@ -409,7 +409,7 @@ fc_status fc_dequantize_cache(fc_handle *h, const fc_cache4 *cache, void *out_k,
  *   sinks     and the first `sinks` are; the others are not read (whole tiles of them).
  * Rows without weight (outside the window, or past a sequence's end) may hold anything.  A sequence without rows gives zeros
  * (a query whose scores are all minus infinity NaN: 0 / 0).  bf16 values past 2^60 may overflow the fp32 sums that are
- * divided at the end.
+ * divided at the end.  Limit: cache rows and tail_capacity together below 2^31 - 4096.
  */
 typedef struct {
   const fc_cache4 *cache4;

@@ -904,7 +904,8 @@ fc_status check_ex(const fc_handle *h, const fc_decode_args *a, const fc_decode_
   if (a->tail_k || a->tail_v || a->tail_len) {
     if (!a->tail_k || !a->tail_v || !a->tail_len || a->tail_capacity < 1) return FC_ERR_INVALID_ARG;
     if (((uintptr_t)a->tail_k & 15) || ((uintptr_t)a->tail_v & 15)) return FC_ERR_INVALID_ARG;
-    if (a->tail_capacity > 0x7fffffff - 4096) return FC_ERR_UNSUPPORTED;
+    // a sequence's rows, kept ones and tail, are counted in 32 bits
+    if ((o->cache4 ? o->cache4->capacity_rows : a->cache_rows) + a->tail_capacity > 0x7fffffffll - 4096) return FC_ERR_UNSUPPORTED;
   }
   return FC_OK;
 }

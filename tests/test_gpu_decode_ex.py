@@ -400,3 +400,21 @@ def test_decode_ex_refusals():
         assert call(_args(), o, ws=None) == WORKSPACE and call(_args(), o, ws=A + 16) == WORKSPACE
         assert call(_args(), o, n=size(_args(), o) - 1) == WORKSPACE
     assert fc._lib.fc_decode_attention_ex(None, ctypes.byref(_args()), ctypes.byref(_opt()), A, A, 1 << 30, None) == INVALID
+
+
+def test_rows_and_tails_past_the_last_int_are_refused():
+    """Kept rows and tail of a sequence are counted together."""
+    h, most = ctypes.create_string_buffer(1 << 16), 0x7fffffff - 4096
+
+    def size(rows, cap, four):
+        a = _args(cache_rows=10 if four else rows, tail_k=A, tail_v=A, tail_len=A, tail_capacity=cap)
+        return fc._lib.fc_decode_workspace_bytes_ex(h, ctypes.byref(a), ctypes.byref(_opt(fc.fc_cache4(A, A, A, A, rows, fc.FC_F16, 2, 128) if four else None)))
+
+    for four in (True, False):
+        rows = most // 16 * 16 - 160
+        assert size(rows, most - rows, four) > 0
+        for cap in (most - rows + 1, 1 << 20, most, 0x7fffffff):
+            assert size(rows, cap, four) == 0
+            a = _args(cache_rows=rows, tail_k=A, tail_v=A, tail_len=A, tail_capacity=cap)
+            o = _opt(fc.fc_cache4(A, A, A, A, rows, fc.FC_F16, 2, 128) if four else None)
+            assert fc._lib.fc_decode_attention_ex(h, ctypes.byref(a), ctypes.byref(o), A, A, 1 << 30, None) == UNSUPPORTED
