@@ -298,7 +298,6 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
   __shared__ WinItem item;                                         // found by one thread while others set up
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid == 0) {
     mbar::init(&sh.qfull, 1u);
     for (int i = 0; i < kSlots; ++i) { mbar::init(&sh.full[i], 1u); mbar::init(&sh.empty[i], 1u); }
@@ -312,6 +311,8 @@ k_window(const __grid_constant__ WinParams P, const __grid_constant__ WinMaps M)
   before_sync();
   __syncthreads();
   after_sync();
+  // Not before this block has its tensor memory: a block of the next kernel that took it would wait for this one to end.
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");             // what the kernels before this one wrote is visible from here
   const unsigned tmem = sh.tmem;                                   // S of tile q at 128 q, O at 128 (NT + q)
   const WinItem &w = item;

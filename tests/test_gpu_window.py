@@ -290,6 +290,27 @@ def test_the_same_call_gives_the_same_bits(handle):
     assert torch.equal(a, b)
 
 
+@pytest.mark.gpu
+def test_calls_of_either_head_size_in_a_row(handle):
+    """Each may begin while the one in front still runs, next to its blocks: the same bits as one by one."""
+    calls = []
+    for d, dtype, nq, nk, Hq, H in ((64, torch.float16, 300, 900, 4, 2), (128, torch.bfloat16, 200, 3000, 8, 2), (64, torch.bfloat16, 5, 4000, 2, 1),
+                                    (128, torch.float16, 70, 70, 2, 2)):
+        q, k, v = _inputs([nq], [nk], Hq, H, d, dtype, nk + d)
+        args = fc.make_window_args(q, k, v, [0, nq], [0, nk], 500, 4)
+        ws = torch.empty(fc.fc_window_workspace_bytes(handle, args), dtype=torch.uint8, device="cuda")
+        want = torch.empty_like(q)
+        fc.fc_window_attention(handle, args, want, ws)
+        torch.cuda.synchronize()
+        calls.append((args, ws, want, (q, k, v)))
+    outs = []
+    for i in range(60):
+        args, ws, want, _ = calls[(i * i + i // 7) % 4]
+        outs.append((torch.empty_like(want), want))
+        fc.fc_window_attention(handle, args, outs[-1][0], ws)
+    assert all(torch.equal(a, b) for a, b in outs) and fc.fc_last_device_status(handle) == 0
+
+
 # ---------------------------------------------------------------------------------------------- refusals, without a GPU
 A = 1 << 20
 
