@@ -267,6 +267,29 @@ def test_halves_of_unlike_scales(handle, size, other, d):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d,G,tails", [(64, 1, None), (128, 7, None), (128, 12, [40])])
+def test_a_row_with_all_the_weight_is_given_back(handle, d, G, tails, dtype):
+    """The largest weight * scale is exact where a reference has just moved to it, so the output is the row's value, off by sums in
+    fp32 (2^-16 of |minimum| + scale * code) and the rounding to the type; the other rows have 2^-60 of the weight."""
+    lens, H, g = [300, 1], 2, torch.Generator().manual_seed(d + G)
+    n = sum(lens)
+    q, k, v = (torch.randn(s, generator=g) for s in ((2, H * G, d), (n, H, d), (n, H, d)))
+    base = torch.randn(d, generator=g)
+    q, k = base + 0.02 * q, 0.02 * k
+    k[77] += base / (base @ base) * 60.0 * math.sqrt(d) * math.log(2.0)
+    q, k, v = (x.to(dtype).cuda() for x in (q, k, v))
+    cache = fc.Cache4.empty(n, H, d, dtype)
+    fc.fc_quantize_cache(handle, k, v, cache)
+    held, size = _held(cache.codes_v, cache.params_v, True)
+    tail = [0.02 * torch.randn((2, 80, H, d), generator=g).to(dtype).cuda() for _ in range(2)] if tails else None
+    out = _run(handle, q, cache, [0, 300, n], tail, tails + [0] if tails else None, 0, 0).double().cpu().numpy()
+    for b, r in ((0, 77), (1, 300)):
+        want, s = (np.repeat(x[r], G, 0) for x in (held, size))
+        assert (np.abs(out[b] - want) <= torch.finfo(dtype).eps / 2 * np.abs(want) + 2.0 ** -16 * s + torch.finfo(dtype).smallest_normal).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_scores_that_are_all_minus_infinity_are_undefined(handle, dtype):
     """0 / 0 by the definition, for the queries and sequences that see nothing else."""
     lens, H, G, d = [40, 300, 2], 2, 4, 64
