@@ -4,9 +4,9 @@
 // rows, then the 16-bit tail.  A step reads every visible row once; the frame is that of fc_decode.cu: the tiles of all
 // sequences and heads form one line, one block per SM takes an equal share of it, a warp keeps a ring of tiles in flight, the
 // other warps only ever wait for the tile they use, blocks that share a sequence meet in a second kernel.
-// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 34.2 us, 3.2 TB/s; 41770 rows of 32 heads 50.0 us, 3.9 TB/s: some
-// 7 us for two launches, the first tile and the joins, the rest bound by the instructions (0.53 a cycle and scheduler, over the
-// whole kernel; a 4-bit row has 3.6 times the arithmetic per byte of a 16-bit one).  A step over 820 rows takes 7.3 us.
+// 189810 rows of 4 heads (4 bits, 7 query heads each, d = 128): 34.4 us, 3.2 TB/s; 41770 rows of 32 heads 50.1 us, 3.9 TB/s: some
+// 7 us for two launches, the first tile and the joins, the rest bound by the instructions (0.54 a cycle and scheduler, over the
+// whole kernel; a 4-bit row has 3.6 times the arithmetic per byte of a 16-bit one).  A step over 820 rows takes 7.4 us.
 //
 //  * A row of 4 bits is 72 bytes of K or V at d = 128 instead of 256.  Nothing is expanded in memory or to fp32:
 //    - codes are masked out of the loaded words and are the tensor cores' operands as they stand, as subnormal half numbers
@@ -21,7 +21,7 @@
 //    largest).  Weight * scale becomes one at a power of two of its own, which a query has for either half of its output and which
 //    follows the largest such product, not the largest weight or the largest scale: the rounding (11 bits, or 2^-33 of that product)
 //    neither overflows nor loses rows beside one whose scale is large and whose weight is not, whatever the range of the cache's
-//    type.  (With one power for all, of the largest scale met: 48.7 instead of 50.0 us over the 41770 rows, 33.4 instead of 36.5
+//    type.  (With one power for all, of the largest scale met: 48.7 instead of 50.1 us over the 41770 rows, 33.4 instead of 36.5
 //    over 100000 rows of 4 heads with 12 query heads each, but a row lost bits from 2^25 times its scale on.)
 //  * Kept rows of 16 bits and tails come in tiles of 32 rows (two warps each, 16 KB at d = 128, about what 128 rows of 4 bits take),
 //    so every tile of the line costs about the same.

@@ -6,7 +6,7 @@
 // tile's scores through it (128 keys at d = 128, in cycles: 2000 from scores to weights, of them 770 + 880 for exponentials, sums and
 // rounding, the rest loads, stores and barriers; 1050 for the products that use them and make the next scores): two such tiles
 // take turns, and the tensor cores have work for 2050 of some 3100 cycles.  32768 tokens of 28 heads over 4 (d = 128, bf16, window
-// 4096): 1.755 ms back to back, where the GPU runs at its power limit, 1.58 ms alone (1030 and 1145 TFLOP/s).
+// 4096): 1.77 ms back to back, where the GPU runs at its power limit, 1.58 ms alone (1020 and 1145 TFLOP/s).
 //
 //  * Queries are taken in tiles of 128 rows, two to a block (one at d = 64) that share one stream of key tiles (128 keys).  A row is a query of one
 //    head; the query heads that share a KV head lie side by side in a tile (128 / G queries each), so keys are read once for
