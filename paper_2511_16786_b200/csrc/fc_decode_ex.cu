@@ -51,8 +51,8 @@ constexpr int kMaxBlocks = 256;                // blocks of a launch, at most
 // Weights are 2^(score - reference).  A reference moves up, so that the largest weight is 2^kReset, where one passes 2^kTop: in 16 bits
 // none overflows then, and weights down to 2^-24 of the largest keep all bits.
 constexpr float kTop = 14.f, kReset = 10.f;
-// Beside 4-bit tiles weights stay in fp32 and are 2^kDown smaller, so that sums of weight * minimum do not overflow, whatever the
-// values are.  There weight * scale is kept to these bounds, by a power of two of its own, kMostUp at most.
+// Beside 4-bit tiles weights stay in fp32 and are 2^kDown smaller, so that sums of weight * minimum over up to 2^18 rows do not
+// overflow, whatever the values are.  There weight * scale is kept to these bounds, by a power of two of its own, kMostUp at most.
 constexpr float kDown = 34.f, kMostUp = 126.f;
 constexpr float kDownPower = 0x1p34f, kMostUpPower = 0x1p126f;
 constexpr float kNothing = -3e38f;             // reference of a query that has seen nothing yet
